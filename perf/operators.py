@@ -1,0 +1,553 @@
+"""One step of a target model over drafted token trees, operator by operator, as timed and checked cases.
+
+Many sequences, each with a paged key / value cache and a tree of drafted tokens whose branches share their first
+tokens, go through the model together.  The step multiplies a few rows with 4-bit weights (``quant``), rotates the
+queries and keys and appends the keys and values to the cache (``append``), attends from every tree row to the cached
+context and to its own ancestors (``tree``), and puts the requests' penalties, biases and grammar masks on the logits
+(``logits``).  Widths are those of the shipped model classes (7B, 32B, 70B in bf16, the tiny fp32 model).
+
+``own`` false: the operators in plain torch operations in 32 bits.  ``own`` true: the framework's entry points.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+# d_model, query heads, key / value heads, head_dim, d_ffn, vocabulary, dtype
+MODELS = {
+    "tiny": (128, 4, 4, 32, 512, 1024, "fp32"),
+    "7b": (3584, 28, 4, 128, 18944, 152064, "bf16"),
+    "32b": (5120, 40, 8, 128, 27648, 152064, "bf16"),
+    "70b": (8192, 64, 8, 128, 28672, 128256, "bf16"),
+}
+ROPE_THETA = 10000.0
+
+
+def listed():
+    return [
+        # One token of one sequence through the QKV projection of the 7B class: the latency of a single decoding step.
+        dict(name="quant-7b-qkv-1", kind="quant", model="7b", proj="qkv", M=1, group=128, zeros=False, epilogue="store"),
+        # A drafted tree of 16 tokens through the widest projection, SwiGLU fused, with a zero point for every group.
+        dict(name="quant-70b-gate-up-16", kind="quant", model="70b", proj="gate_up", M=16, group=128, zeros=True, epilogue="swiglu"),
+        # 61 rows of a batch through the down projection, added to the fp32 residual stream; small groups, no size a multiple of a tile.
+        dict(name="quant-7b-down-61", kind="quant", model="7b", proj="down", M=61, group=64, zeros=True, epilogue="residual"),
+        # 16 sequences append one token each: rows of 7B heads scattered over as many pages.
+        dict(name="append-7b-tokens-16", kind="append", model="7b", seqs=16, rows_min=1, rows_max=1, cached_min=100, cached_max=4000, page=16,
+             layout="half", rot=128),
+        # A prompt of 4093 tokens in one call; interleaved pairs in half of every head.
+        dict(name="append-70b-prompt", kind="append", model="70b", seqs=1, rows_min=4093, rows_max=4093, cached_min=0, cached_max=0, page=64,
+             layout="interleaved", rot=64),
+        # The tiny fp32 model: a handful of small trees.
+        dict(name="append-tiny-trees", kind="append", model="tiny", seqs=5, rows_min=1, rows_max=23, cached_min=0, cached_max=300, page=16,
+             layout="half", rot=32),
+        # One drafted tree of 16 tokens behind a short prompt of the 7B class: the smallest attention of a step.
+        dict(name="tree-7b-16", kind="tree", model="7b", seqs=1, rows_min=16, rows_max=16, cached_min=512, cached_max=512, page=16,
+             softcap=0.0, window=0),
+        # A single token over a context of 131,071 tokens: the cache read once.
+        dict(name="tree-70b-long", kind="tree", model="70b", seqs=1, rows_min=1, rows_max=1, cached_min=131071, cached_max=131071, page=64,
+             softcap=0.0, window=0),
+        # A serving batch: 24 sequences of very different lengths, trees of up to 64 tokens, scores capped, a sliding window.
+        dict(name="tree-32b-batch", kind="tree", model="32b", seqs=24, rows_min=1, rows_max=64, cached_min=0, cached_max=12000, page=32,
+             softcap=30.0, window=4096),
+        # One row, 152,064 logits, a history of 2000 tokens: the end of a single decoding step.
+        dict(name="logits-7b-1", kind="logits", model="7b", dtype="fp32", seqs=1, rows_min=1, rows_max=1, history_min=2000, history_max=2000,
+             bias=20, mask=False),
+        # Trees of 16 sequences, up to 16 rows each, under a grammar.
+        dict(name="logits-7b-trees", kind="logits", model="7b", dtype="fp32", seqs=16, rows_min=3, rows_max=16, history_min=1, history_max=8000,
+             bias=100, mask=True),
+        # 256 single tokens with bf16 logits and long histories.
+        dict(name="logits-70b-256", kind="logits", model="70b", dtype="bf16", seqs=256, rows_min=1, rows_max=1, history_min=0, history_max=32000,
+             bias=0, mask=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["quant", "quant", "append", "tree", "tree", "logits"])
+    if kind == "quant":
+        model = rng.choice(["tiny", "7b", "7b", "32b", "70b"])
+        proj, epilogue = rng.choice([("qkv", "store"), ("qkv", "store_f32"), ("o", "residual"), ("gate_up", "swiglu"), ("down", "residual")])
+        return dict(kind=kind, model=model, proj=proj, M=_log(rng, 1, 16 if proj == "gate_up" and model == "70b" else 64),
+                    group=32 if model == "tiny" else rng.choice([32, 64, 128]), zeros=rng.random() < 0.5, epilogue=epilogue)
+    if kind == "append":
+        model, big = rng.choice(["tiny", "7b", "32b", "70b"]), _log(rng, 1, 2000)
+        hd = MODELS[model][3]
+        return dict(kind=kind, model=model, seqs=1 if big > 128 else rng.randint(1, 24), rows_min=max(1, big // 2), rows_max=big,
+                    cached_min=0, cached_max=_log(rng, 10, 4000), page=rng.choice([16, 32, 64]), layout=rng.choice(["half", "interleaved"]), rot=rng.choice([hd, hd // 2]))
+    if kind == "tree":
+        model, seqs, n = rng.choice(["tiny", "7b", "32b", "70b"]), _log(rng, 1, 24), _log(rng, 1, 64)
+        longest = _log(rng, 16, 120000 // seqs)
+        return dict(kind=kind, model=model, seqs=seqs, rows_min=max(1, n // 4), rows_max=n, cached_min=longest // 3, cached_max=longest,
+                    page=rng.choice([16, 32, 64]), softcap=rng.choice([0.0, 0.0, 30.0]), window=rng.choice([0, 0, _log(rng, 16, 4096)]))
+    seqs = _log(rng, 1, 64)
+    n = _log(rng, 1, max(1, 200 // seqs))
+    return dict(kind=kind, model=rng.choice(["tiny", "7b", "70b"]), dtype=rng.choice(["fp32", "bf16"]), seqs=seqs, rows_min=max(1, n // 2), rows_max=n,
+                history_min=0, history_max=_log(rng, 1, 32000), bias=rng.choice([0, 30]), mask=rng.random() < 0.5)
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(1000003 * int(seed) + 29)
+
+
+def _dtype(case):
+    name = case.get("dtype") or MODELS[case["model"]][6]
+    return torch.float32 if name == "fp32" else torch.bfloat16
+
+
+def _shape(case):
+    """N (output features), K of a projection"""
+    d, nq, nkv, hd, ffn, _, _ = MODELS[case["model"]]
+    return {"qkv": ((nq + 2 * nkv) * hd, d), "o": (d, nq * hd), "gate_up": (ffn, d), "down": (d, ffn)}[case["proj"]]
+
+
+def _lens(case, key):
+    """The lengths of a case's sequences: part of the case, spread evenly between its limits and shuffled."""
+    lo, hi = case[key + "_min"], case[key + "_max"]
+    n = case["seqs"]
+    lens = [lo + (hi - lo) * (2 * i + 1) // (2 * n) for i in range(n)] if n > 1 else [hi]
+    random.Random(n * 131 + hi).shuffle(lens)
+    return lens
+
+
+def _trees(case, seed):
+    """The parents of every drafted token (index inside its own tree, -1: it follows the context), and their depths."""
+    rng, parents, depths = random.Random(seed * 7919 + case["seqs"]), [], []
+    for n in _lens(case, "rows"):
+        chain = n > 256                                     # a prompt, not a drafted tree
+        p = [i - 1 if chain or rng.random() < 0.6 else rng.randint(-1, i - 1) for i in range(n)]
+        d = []
+        for i in range(n):
+            d.append(d[p[i]] + 1 if p[i] >= 0 else 0)
+        parents.append(p)
+        depths.append(d)
+    return parents, depths
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _offsets(lens):
+    out = [0]
+    for n in lens:
+        out.append(out[-1] + n)
+    return out
+
+
+def _randn(g, *shape, dtype=torch.float32):
+    return torch.randn(*shape, device="cuda", generator=g).to(dtype)
+
+
+def _quant_inputs(case, seed):
+    g, dt = _gen(seed), _dtype(case)
+    N, K = _shape(case)
+    rows, G = (2 * N if case["epilogue"] == "swiglu" else N), case["group"]
+    s = {"x": _randn(g, case["M"], K, dtype=dt)}
+    s["codes"] = torch.randint(0, 256, (rows, K // 2), dtype=torch.uint8, device="cuda", generator=g)
+    s["scales"] = ((0.5 + torch.rand(rows, K // G, device="cuda", generator=g)) / (4.6 * math.sqrt(K))).to(dt)
+    s["zeros"] = torch.randint(6, 11, (rows, K // G), dtype=torch.uint8, device="cuda", generator=g) if case["zeros"] else None
+    s["residual"] = _randn(g, case["M"], N) if case["epilogue"] == "residual" else None
+    return s
+
+
+def _paged_inputs(case, seed, g):
+    """A paged cache that holds every sequence's context and has room for its new rows; pages in no order."""
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    dt, page = _dtype(case), case["page"]
+    cached, rows = _lens(case, "cached"), _lens(case, "rows")
+    need = [-(-(c + n) // page) for c, n in zip(cached, rows)]
+    total, width = sum(need), max(need)
+    order = torch.randperm(total, device="cuda", generator=g).to(torch.int32)
+    table = torch.zeros(len(need), width, dtype=torch.int32, device="cuda")
+    for i, (first, n) in enumerate(zip(_offsets(need), need)):
+        table[i, :n] = order[first:first + n]
+    parents, depths = _trees(case, seed)
+    return {"k_pages": _randn(g, total, nkv, page, hd, dtype=dt), "v_pages": _randn(g, total, nkv, hd, page, dtype=dt), "table": table,
+            "cached": _i32(cached), "row_offsets": _i32(_offsets(rows)), "lens": (cached, rows),
+            "parents": _i32([p for tree in parents for p in tree]), "depth": 1 + max(d for tree in depths for d in tree),
+            "positions": _i32([c + d for c, tree in zip(cached, depths) for d in tree])}
+
+
+def _append_inputs(case, seed):
+    g = _gen(seed)
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    s = _paged_inputs(case, seed, g)
+    R, half = sum(s["lens"][1]), case["rot"] // 2
+    s["qkv"] = _randn(g, R, (nq + 2 * nkv) * hd, dtype=_dtype(case))
+    most = max(c + n for c, n in zip(*s["lens"]))
+    ang = torch.arange(most, dtype=torch.float64, device="cuda")[:, None] * ROPE_THETA ** (-torch.arange(half, dtype=torch.float64, device="cuda") / half)
+    s["rotary"] = torch.stack([torch.cos(ang), torch.sin(ang)], dim=-1).float()            # kept by the program from its start
+    return s
+
+
+def _tree_inputs(case, seed):
+    g = _gen(seed)
+    _, nq, _, hd, _, _, _ = MODELS[case["model"]]
+    s = _paged_inputs(case, seed, g)
+    s["q"] = _randn(g, sum(s["lens"][1]), nq * hd, dtype=_dtype(case)) * 1.5               # some keys stand out
+    return s
+
+
+def _logits_inputs(case, seed):
+    g, V, dt = _gen(seed), MODELS[case["model"]][5], _dtype(case)
+    rows, hist = _lens(case, "rows"), _lens(case, "history")
+    R, S = sum(rows), case["seqs"]
+    tokens = lambda n: (V * torch.rand(n, device="cuda", generator=g) ** 4).long().clamp_(max=V - 1).to(torch.int32)      # a few words are common
+    parents, depths = _trees(case, seed)
+    u = lambda lo, hi: lo + (hi - lo) * torch.rand(S, device="cuda", generator=g)
+    s = {"logits": (2.5 * torch.randn(R, V, device="cuda", generator=g)).to(dt), "row_offsets": _i32(_offsets(rows)), "lens": rows,
+         "params": torch.stack([u(1.0, 1.3), u(0.0, 0.5), u(0.0, 0.5), u(0.6, 1.2)], dim=1).contiguous(),
+         "history": tokens(sum(hist)), "history_offsets": _i32(_offsets(hist)), "prompt_lens": _i32([n // 2 for n in hist]), "history_lens": hist,
+         "tree_ids": tokens(R), "parents": _i32([p for tree in parents for p in tree]), "depth": 1 + max(d for tree in depths for d in tree),
+         "bias_ids": None, "bias_values": None, "bias_offsets": None, "mask": None}
+    n = case["bias"]
+    if n:
+        s["bias_ids"] = torch.cat([torch.randperm(V, device="cuda", generator=g)[:n] for _ in range(S)]).to(torch.int32)
+        s["bias_values"] = _randn(g, S * n) * 3.0
+        s["bias_offsets"] = _i32([n * i for i in range(S + 1)])
+    if case["mask"]:
+        words = -(-V // 32)
+        s["mask"] = torch.empty(R, words, dtype=torch.int32, device="cuda")
+        weight = (1 << torch.arange(32, dtype=torch.int64, device="cuda"))
+        for r in range(R):                                  # after some tokens nearly all may follow, after others a few
+            share = (0.95, 0.5, 0.002)[r % 3]
+            bits = (torch.rand(words, 32, device="cuda", generator=g) < share).long()
+            s["mask"][r] = (bits * weight).sum(dim=1).to(torch.int32)
+    return s
+
+
+_INPUTS = {"quant": _quant_inputs, "append": _append_inputs, "tree": _tree_inputs, "logits": _logits_inputs}
+
+
+def _empty(*shape, dtype=torch.float32):
+    return torch.empty(*shape, dtype=dtype, device="cuda")
+
+
+def prepare(case, seed):
+    kind, dt = case["kind"], _dtype(case)
+    s = _INPUTS[kind](case, seed)
+    s["case"] = dict(case)
+    _, nq, nkv, hd, _, V, _ = MODELS[case["model"]]
+    if kind == "quant":
+        s["out"] = _empty(case["M"], _shape(case)[0], dtype=torch.float32 if case["epilogue"] in ("residual", "store_f32") else dt)
+    elif kind == "append":
+        s["q_out"] = _empty(s["qkv"].shape[0], nq * hd, dtype=dt)
+    elif kind == "tree":
+        s["out"] = _empty(s["q"].shape[0], nq * hd, dtype=dt)
+    else:
+        R = s["logits"].shape[0]
+        s.update(out=_empty(R, V, dtype=dt), top=_empty(R, dtype=torch.int32), lse=_empty(R))
+    if own:
+        import paper_2509_15148_amd as A
+        if kind in ("append", "tree"):
+            s["cache"] = A.PagedCache(s["k_pages"], s["v_pages"], s["table"])
+        if kind == "tree":
+            need = A.atts_attention_tree_workspace_bytes(s["cache"], nq, s["q"].shape[0], max(s["lens"][1]), max(s["lens"][0]))
+            s["ws"] = _empty(max(256, need), dtype=torch.uint8)
+        if kind == "logits":
+            s["ws"] = _empty(max(256, A.atts_logits_adjust_workspace_bytes(s["logits"].shape[0], V)), dtype=torch.uint8)
+    return s
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------
+
+def run(s):
+    return (_run_own if own else _run_plain)(s, s["case"])
+
+
+def _run_own(s, case):
+    import paper_2509_15148_amd as A
+    kind = case["kind"]
+    if kind == "quant":
+        epilogue = {"store": A.EPILOGUE_STORE, "store_f32": A.EPILOGUE_STORE_F32, "residual": A.EPILOGUE_RESIDUAL, "swiglu": A.EPILOGUE_SWIGLU}
+        A.atts_gemm_nt_quant(s["x"], s["codes"], s["scales"], s["zeros"], s["out"], epilogue[case["epilogue"]], s["residual"])
+        return s["out"]
+    if kind == "append":
+        layout = A.ROTARY_HALF if case["layout"] == "half" else A.ROTARY_INTERLEAVED
+        A.atts_rotary_append(s["cache"], s["qkv"], s["positions"], s["cached"], s["row_offsets"], s["rotary"], layout, s["q_out"])
+        return {"q": s["q_out"], "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
+    if kind == "tree":
+        cached, rows = s["lens"]
+        A.atts_attention_tree(s["cache"], s["q"], s["parents"], s["cached"], s["row_offsets"], max(rows), max(cached), s["out"], s["ws"],
+                              softcap=case["softcap"], window=case["window"])
+        return s["out"]
+    A.atts_logits_adjust(s["logits"], s["row_offsets"], s["params"], s["history"], s["history_offsets"], s["prompt_lens"], s["tree_ids"], s["parents"],
+                         s["bias_ids"], s["bias_values"], s["bias_offsets"], s["mask"], s["out"], s["top"], s["lse"], s["ws"])
+    return {"logits": s["out"], "top": s["top"], "lse": s["lse"]}
+
+
+def _run_plain(s, case):
+    return {"quant": _plain_quant, "append": _plain_append, "tree": _plain_tree, "logits": _plain_logits}[case["kind"]](s, case)
+
+
+def _plain_quant(s, case):
+    codes = s["codes"]
+    q = torch.stack([codes & 15, codes >> 4], dim=-1).reshape(codes.shape[0], s["scales"].shape[1], case["group"]).float()
+    q = q - (8.0 if s["zeros"] is None else s["zeros"].float()[:, :, None])
+    w = (q * s["scales"].float()[:, :, None]).reshape(codes.shape[0], -1)
+    y = s["x"].float() @ w.t()
+    if case["epilogue"] == "swiglu":
+        gate, up = y[:, :y.shape[1] // 2], y[:, y.shape[1] // 2:]
+        y = gate / (1.0 + torch.exp(-gate)) * up
+    if case["epilogue"] == "residual":
+        y = s["residual"] + y
+    s["out"].copy_(y)
+    return s["out"]
+
+
+def _sequences(s, device):
+    """Sequence and index inside it of every new row"""
+    rows = s["lens"][1] if isinstance(s["lens"], tuple) else s["lens"]
+    offsets = s["row_offsets"].long()
+    seq = torch.repeat_interleave(torch.arange(len(rows), device=device), offsets[1:] - offsets[:-1], output_size=sum(rows))
+    return seq, torch.arange(sum(rows), device=device) - offsets[seq], offsets
+
+
+def _plain_append(s, case):
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    x = s["qkv"].float()
+    x = x.reshape(x.shape[0], nq + 2 * nkv, hd)
+    t = s["rotary"][s["positions"].long()][:, None]
+    c, sn, rot = t[..., 0], t[..., 1], case["rot"]
+    qk = x[:, :nq + nkv]
+    if case["layout"] == "half":
+        a, b = qk[..., :rot // 2], qk[..., rot // 2:rot]
+        turned = torch.cat([a * c - b * sn, b * c + a * sn, qk[..., rot:]], dim=-1)
+    else:
+        a, b = qk[..., 0:rot:2], qk[..., 1:rot:2]
+        turned = torch.cat([torch.stack([a * c - b * sn, b * c + a * sn], dim=-1).flatten(-2), qk[..., rot:]], dim=-1)
+    s["q_out"].copy_(turned[:, :nq].reshape(x.shape[0], -1))
+    seq, local, _ = _sequences(s, x.device)
+    at = s["cached"].long()[seq] + local
+    page, slot = s["table"][seq, at // case["page"]].long(), at % case["page"]
+    s["k_pages"][page, :, slot] = turned[:, nq:].to(s["k_pages"].dtype)
+    s["v_pages"][page, :, :, slot] = x[:, nq + nkv:].to(s["v_pages"].dtype)
+    return {"q": s["q_out"], "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
+
+
+def _ancestors(s, seq, local, offsets, columns):
+    """[rows, columns]: column j of a row is true if tree token j is the row itself or one it descends from"""
+    parents, at = s["parents"].long(), local.clone()
+    columns = torch.arange(columns, device=local.device)[None, :]
+    seen = torch.zeros(local.numel(), columns.numel(), dtype=torch.bool, device=local.device)
+    for _ in range(s["depth"]):
+        seen |= at[:, None] == columns
+        at = torch.where(at >= 0, parents[offsets[seq] + at.clamp(min=0)], at)
+    return seen
+
+
+def _plain_tree(s, case):
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    page, group = case["page"], nq // nkv
+    cached, rows = s["lens"]
+    seq, local, offsets = _sequences(s, s["q"].device)
+    seen = _ancestors(s, seq, local, offsets, max(rows))
+    depth = seen.sum(dim=1) - 1
+    first = _offsets(rows)
+    for i, (L, n) in enumerate(zip(cached, rows)):
+        r, m = slice(first[i], first[i] + n), L + n
+        pages = s["table"][i, :-(-m // page)].long()
+        k = s["k_pages"][pages].float().transpose(0, 1).reshape(nkv, -1, hd)[:, :m]
+        v = s["v_pages"][pages].float().permute(1, 0, 3, 2).reshape(nkv, -1, hd)[:, :m]
+        q = s["q"][r].float().reshape(n, nkv, group, hd).transpose(0, 1).reshape(nkv, n * group, hd)
+        z = (q @ k.transpose(1, 2)).reshape(nkv, n, group, m) / math.sqrt(hd)
+        if case["softcap"]:
+            z = case["softcap"] * torch.tanh(z / case["softcap"])
+        open_ = torch.cat([torch.ones(n, L, dtype=torch.bool, device=q.device), seen[r, :n]], dim=1)
+        if case["window"]:
+            at = torch.cat([torch.arange(L, device=q.device), L + depth[r]])
+            open_ = open_ & ((L + depth[r])[:, None] - at[None, :] < case["window"])
+        z = torch.where(open_[None, :, None, :], z, torch.full_like(z, -math.inf))
+        p = torch.exp(z - z.amax(dim=-1, keepdim=True))
+        p = (p / p.sum(dim=-1, keepdim=True)).reshape(nkv, n * group, m)
+        s["out"][r] = (p @ v).reshape(nkv, n, group, hd).transpose(0, 1).reshape(n, nq * hd).to(s["out"].dtype)
+    return s["out"]
+
+
+def _plain_logits(s, case):
+    x = s["logits"].float()
+    R, V = x.shape
+    seq, local, offsets = _sequences(s, x.device)
+    # tokens of the prompt, and how often each was generated: history behind the prompt, and the row's own path in the tree
+    hist, ho = s["history"].long(), s["history_offsets"].long()
+    owner = torch.repeat_interleave(torch.arange(case["seqs"], device=x.device), ho[1:] - ho[:-1], output_size=hist.numel())
+    made = (torch.arange(hist.numel(), device=x.device) - ho[owner] >= s["prompt_lens"].long()[owner]).float()
+    table = torch.zeros(2, case["seqs"] * V, device=x.device)
+    table[0].index_add_(0, owner * V + hist, 1.0 - made)
+    table[1].index_add_(0, owner * V + hist, made)
+    prompt, count = table.reshape(2, case["seqs"], V)[:, seq]
+    at, ids, parents = local.clone(), s["tree_ids"].long(), s["parents"].long()
+    for _ in range(s["depth"]):
+        node = offsets[seq] + at.clamp(min=0)
+        count.scatter_add_(1, ids[node][:, None], (at >= 0).float()[:, None])
+        at = torch.where(at >= 0, parents[node], at)
+    rep, freq, pres, temp = (p[seq][:, None] for p in s["params"].unbind(1))
+    x = torch.where(prompt + count > 0, torch.where(x > 0, x / rep, x * rep), x)
+    x = x - count * freq
+    x = torch.where(count > 0, x - pres, x)
+    if s["bias_ids"] is not None:
+        bo, b = s["bias_offsets"].long(), s["bias_ids"].long()
+        owner = torch.repeat_interleave(torch.arange(case["seqs"], device=x.device), bo[1:] - bo[:-1], output_size=b.numel())
+        bias = torch.zeros(case["seqs"], V, device=x.device)
+        bias[owner, b] = s["bias_values"]
+        x = x + bias[seq]
+    x = x / temp
+    if s["mask"] is not None:
+        v = torch.arange(V, device=x.device)
+        x = torch.where((s["mask"][:, v // 32] >> (v % 32)) & 1 != 0, x, torch.full_like(x, -math.inf))
+    s["out"].copy_(x)
+    top = x.amax(dim=1, keepdim=True)
+    first = torch.where(x == top, torch.arange(V, device=x.device), V).amin(dim=1)          # ties: the lowest index
+    s["top"].copy_(torch.where(top[:, 0] > -math.inf, first, -1))
+    s["lse"].copy_(top[:, 0] + torch.log(torch.exp(x - top).sum(dim=1)))
+    return {"logits": s["out"], "top": s["top"], "lse": s["lse"]}
+
+
+# ---- what a pass cannot do without ----------------------------------------------------------------------------------
+
+def work(case):
+    kind, es = case["kind"], 4 if _dtype(case) == torch.float32 else 2
+    _, nq, nkv, hd, _, V, _ = MODELS[case["model"]]
+    if kind == "quant":
+        N, K = _shape(case)
+        wide = 2 * N if case["epilogue"] == "swiglu" else N
+        out = {"store": es, "swiglu": es, "store_f32": 4, "residual": 8}[case["epilogue"]]
+        return {"bytes": wide * K * 0.5 + wide * (K // case["group"]) * (es + (1 if case["zeros"] else 0)) + es * case["M"] * K + out * case["M"] * N,
+                "flops": 2.0 * case["M"] * wide * K}
+    rows = _lens(case, "rows")
+    R = sum(rows)
+    if kind == "append":
+        return {"bytes": 2.0 * es * R * (nq + 2 * nkv) * hd + R * (4.0 * case["rot"] + 4.0), "flops": 3.0 * R * (nq + nkv) * case["rot"]}
+    if kind == "tree":
+        keys = pairs = 0
+        for L, n in zip(_lens(case, "cached"), rows):
+            seen = min(L, case["window"] - 1) if case["window"] else L
+            keys += seen + n
+            pairs += n * (seen + min(n, 4))                 # a drafted token has a few ancestors
+        return {"bytes": es * (2.0 * keys * nkv + 2.0 * R * nq) * hd, "flops": 4.0 * nq * hd * pairs}
+    history = sum(_lens(case, "history"))
+    return {"bytes": 2.0 * es * R * V + 4.0 * history + 8.0 * case["bias"] * case["seqs"] + (R * V / 8.0 if case["mask"] else 0.0) + 16.0 * R,
+            "flops": 8.0 * R * V}
+
+
+# ---- the same in 64 bits --------------------------------------------------------------------------------------------
+
+def exact(case, seed):
+    s = _INPUTS[case["kind"]](case, seed)
+    return {"quant": _exact_quant, "append": _exact_append, "tree": _exact_tree, "logits": _exact_logits}[case["kind"]](s, case, seed)
+
+
+def _exact_quant(s, case, seed):
+    G, x = case["group"], s["x"].double()
+    rows, groups = s["scales"].shape
+    y = torch.zeros(case["M"], rows, dtype=torch.float64, device="cuda")
+    for g in range(groups):                                 # one group of inputs after the other, its scale behind the sum
+        byte = s["codes"][:, g * G // 2:(g + 1) * G // 2].double()
+        high = torch.floor(byte / 16.0)
+        zero = 8.0 if s["zeros"] is None else s["zeros"][:, g, None].double()
+        xs = x[:, g * G:(g + 1) * G]
+        part = xs[:, 0::2].contiguous() @ (byte - 16.0 * high - zero).t() + xs[:, 1::2].contiguous() @ (high - zero).t()
+        y += part * s["scales"][:, g].double()
+    if case["epilogue"] == "swiglu":
+        gate, up = y.chunk(2, dim=1)
+        y = gate * torch.sigmoid(gate) * up
+    return y + s["residual"].double() if case["epilogue"] == "residual" else y
+
+
+def _exact_append(s, case, seed):
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    rot, page = case["rot"], case["page"]
+    x = s["qkv"].double().reshape(-1, nq + 2 * nkv, hd)
+    pairs = s["rotary"].double()[s["positions"].long()]
+    turn = torch.view_as_complex(pairs.contiguous())[:, None]
+    first = torch.arange(rot // 2, device="cuda") * (1 if case["layout"] == "half" else 2)
+    second = first + (rot // 2 if case["layout"] == "half" else 1)
+    z = torch.complex(x[..., first], x[..., second]) * turn
+    y = x.clone()
+    y[:, :nq + nkv, first] = z.real[:, :nq + nkv]
+    y[:, :nq + nkv, second] = z.imag[:, :nq + nkv]
+    k, v, table = s["k_pages"].double(), s["v_pages"].double(), s["table"].tolist()
+    r, pages, slots = 0, [], []
+    for i, (L, n) in enumerate(zip(*s["lens"])):
+        pages += [table[i][j // page] for j in range(L, L + n)]
+        slots += [j % page for j in range(L, L + n)]
+    pages, slots = torch.tensor(pages, device="cuda"), torch.tensor(slots, device="cuda")
+    k[pages, :, slots] = y[:, nq:nq + nkv]
+    v[pages, :, :, slots] = y[:, nq + nkv:]
+    return {"q": y[:, :nq].reshape(y.shape[0], -1), "k_pages": k, "v_pages": v}
+
+
+def _exact_tree(s, case, seed):
+    _, nq, nkv, hd, _, _, _ = MODELS[case["model"]]
+    page, group = case["page"], nq // nkv
+    parents, depths = _trees(case, seed)
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda")
+    r0 = 0
+    for i, (L, n) in enumerate(zip(*s["lens"])):
+        see = torch.zeros(n, L + n, dtype=torch.bool)
+        see[:, :L] = True
+        for t in range(n):
+            a = t
+            while a >= 0:
+                see[t, L + a] = True
+                a = parents[i][a]
+        if case["window"]:
+            at = torch.tensor(list(range(L)) + [L + d for d in depths[i]])
+            see &= at[L:, None] < at[None, :] + case["window"]
+        see = see.cuda()
+        pages = s["table"][i, :(L + n + page - 1) // page].long()
+        for h in range(nkv):
+            k = s["k_pages"][pages, h].double().reshape(-1, hd)[:L + n]
+            v = s["v_pages"][pages, h].double().transpose(1, 2).reshape(-1, hd)[:L + n]
+            for j in range(h * group, (h + 1) * group):
+                z = s["q"][r0:r0 + n, j * hd:(j + 1) * hd].double() @ k.t() * hd ** -0.5
+                if case["softcap"]:
+                    z = torch.tanh(z / case["softcap"]) * case["softcap"]
+                out[r0:r0 + n, j * hd:(j + 1) * hd] = torch.softmax(z.masked_fill_(~see, -math.inf), dim=1) @ v
+        r0 += n
+    return out
+
+
+def _exact_logits(s, case, seed):
+    x = s["logits"].double()
+    parents, _ = _trees(case, seed)
+    params, r = s["params"].double().tolist(), 0
+    hist, ho, split = s["history"].long(), s["history_offsets"].tolist(), s["prompt_lens"].tolist()
+    lse, V = [], x.shape[1]
+    for i, n in enumerate(s["lens"]):
+        rep, freq, pres, temp = params[i]
+        own_tokens = hist[ho[i]:ho[i + 1]]
+        prompt, base = own_tokens[:split[i]], torch.bincount(own_tokens[split[i]:], minlength=V).double()
+        tree = s["tree_ids"][r:r + n].long()
+        for t in range(n):
+            path, a = [], t
+            while a >= 0:
+                path.append(a)
+                a = parents[i][a]
+            count = base + torch.bincount(tree[path], minlength=V)
+            known = count > 0
+            known[prompt] = True
+            row = x[r + t]
+            row = torch.where(known, torch.where(row > 0, row / rep, row * rep), row) - count * freq - (count > 0).double() * pres
+            if s["bias_ids"] is not None:
+                lo, hi = case["bias"] * i, case["bias"] * (i + 1)
+                row[s["bias_ids"][lo:hi].long()] += s["bias_values"][lo:hi].double()
+            row = row / temp
+            if s["mask"] is not None:
+                word = s["mask"][r + t].long()[:, None] & 0xFFFFFFFF
+                shut = (torch.bitwise_right_shift(word, torch.arange(32, device="cuda")) % 2 == 0).reshape(-1)[:V]
+                row = row.masked_fill(shut, -math.inf)
+            x[r + t] = row
+            lse.append(torch.logsumexp(row, dim=0))
+        r += n
+    # the arg max belongs to the rounded values: the best two can be nearer to each other than a rounding
+    return {"logits": x, "top": None, "lse": torch.stack(lse)}
