@@ -281,7 +281,7 @@ def _run_own(s, case):
                               softcap=case["softcap"], window=case["window"])
         return s["out"]
     A.atts_logits_adjust(s["logits"], s["row_offsets"], s["params"], s["history"], s["history_offsets"], s["prompt_lens"], s["tree_ids"], s["parents"],
-                         s["bias_ids"], s["bias_values"], s["bias_offsets"], s["mask"], s["out"], s["top"], s["lse"], s["ws"])
+                         s["bias_ids"], s["bias_values"], s["bias_offsets"], s["mask"], s["out"], s["top"], s["lse"], s["ws"], max_rows=max(s["lens"]))
     return {"logits": s["out"], "top": s["top"], "lse": s["lse"]}
 
 
