@@ -428,6 +428,142 @@ int32_t atts_classic_threshold(const float* cal_scores, int64_t n_scores, double
                                size_t workspace_bytes, void* hip_stream);
 int32_t atts_classic_prediction_sets(const float* scores, int64_t count, const float* tau, uint8_t* member, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------
+ * One step of the target model over drafted token trees ("Verification" and "Target Model Sampling" for many
+ * requests at once): every sequence brings a paged key / value cache and new rows, which are the drafted tokens of a
+ * tree (branches share their first tokens), or the one token of an ordinary decoding step, or a prompt.  The operators of such a step:
+ *
+ *   atts_gemm_nt_quant    projections of a few rows with weights in 4 bits
+ *   atts_rotary_append    rotary embedding of queries and keys, keys and values appended to the cache
+ *   atts_attention_tree   attention of the new rows to the cached context and to their own ancestors
+ *   atts_logits_adjust    penalties, biases, temperature and a grammar mask on the logits, with the arg max and the log-sum-exp
+ *
+ * Rows and trees.  The rows of all sequences lie one behind the other: sequence s has rows row_offsets[s] .. row_offsets[s + 1] - 1
+ * (dev int32 [n_seqs + 1], non-decreasing, first entry 0), possibly none.  parents dev int32 [R] holds for every row the index, inside its own
+ * sequence's rows, of the row it follows, or -1 for a row that follows the context; a parent comes before its children.  An entry
+ * outside [-1, own index) is read as -1.  A tree has at most ATTS_MAX_TREE rows.
+ *
+ * The paged cache.  Keys lie as rows, values transposed, which is how the attention kernels feed them to the matrix cores:
+ *   k_pages    dev [n_pages, n_kv_heads, page_rows, head_dim]      (dtype), 16-byte aligned
+ *   v_pages    dev [n_pages, n_kv_heads, head_dim, page_rows]      (dtype), 16-byte aligned
+ *   page_table dev int32 [n_seqs, max_pages]: token j of sequence s lies in slot j % page_rows of page page_table[s][j / page_rows]
+ * page_rows is a power of two in [8, 4096], head_dim a multiple of 8, at most 256.  The struct is read during a call only.
+ * `cached` dev int32 [n_seqs] is the number of tokens each sequence held before the step; new row i of sequence s becomes token
+ * cached[s] + i of its cache.  Lengths and tables are read on the device; values out of range never fault: tokens
+ * beyond max_pages pages do not exist, a row whose page is outside [0, n_pages) is not stored, and such a page is read as page 0.
+ * ---------------------------------------------------------------------------------- */
+#define ATTS_MAX_TREE 256
+
+typedef struct {
+    void*          k_pages;
+    void*          v_pages;
+    const int32_t* page_table;
+    int32_t dtype, n_pages, page_rows, n_kv_heads, head_dim, n_seqs, max_pages;
+} atts_paged_cache;
+
+/* out = X W^T with W[n, k] = scales[n, k / group] (code(n, k) - zeros[n, k / group]) in 4 bits: the product of a few rows with a
+ * weight matrix that is read once.  Sums are held in 32 bits; a code times an activation is exact.
+ *   x         dev [M, Kdim] (dtype), rows x_stride elements apart, 16-byte aligned, x_stride * sizeof(dtype) a multiple of 16
+ *   codes     dev uint8 [rows, Kdim / 2], 16-byte aligned: code k of a row is the low (k even) or high half of byte k / 2
+ *   scales    dev [rows, Kdim / group] (dtype);  zeros dev uint8 [rows, Kdim / group], or NULL: 8 everywhere
+ *   group     32, 64 or 128; divides Kdim
+ *   epilogue  ATTS_EPILOGUE_STORE      out (dtype) [M, N] = product                         (rows of W: N)
+ *             ATTS_EPILOGUE_STORE_F32  out (float) [M, N] = product
+ *             ATTS_EPILOGUE_RESIDUAL   out (float) [M, N] = residual + product; residual dev float [M, N], out may be the same array
+ *             ATTS_EPILOGUE_SWIGLU     out (dtype) [M, N] = silu(gate) * up                 (rows of W: N gate rows, then N up rows)
+ * M >= 0 (0 is a no-op), N >= 1.  Meant for up to about a hundred rows: the weights are read once for every 64. */
+#define ATTS_EPILOGUE_STORE     0
+#define ATTS_EPILOGUE_STORE_F32 1
+#define ATTS_EPILOGUE_RESIDUAL  2
+#define ATTS_EPILOGUE_SWIGLU    3
+int32_t atts_gemm_nt_quant(int32_t dtype, const void* x, int64_t x_stride, const uint8_t* codes, const void* scales, const uint8_t* zeros,
+                           int32_t group, const float* residual, void* out, int32_t M, int32_t N, int32_t Kdim, int32_t epilogue,
+                           void* hip_stream);
+
+/* Codes, scales and zeros of a matrix w dev [N, Kdim] (dtype) for atts_gemm_nt_quant, group by group.  With lo = min(0, smallest) and hi =
+ * max(0, largest) value of the group:
+ *   zeros != NULL  scale = (hi - lo) / 15,           zero = round(-lo / scale)
+ *   zeros == NULL  scale = max(-lo / 8, hi / 7),     zero = 8
+ * code = min(max(round(w / scale) + zero, 0), 15), round half to even, in 32 bits with the scale as it is stored; a group of zeros gets
+ * scale 0 and the code of zero.  Values have to be finite. */
+int32_t atts_quantize_rows(int32_t dtype, const void* w, int32_t N, int32_t Kdim, int32_t group, uint8_t* codes, void* scales, uint8_t* zeros,
+                           void* hip_stream);
+
+/* The rotary table for positions first .. first + rows - 1: table dev float [rows, rot_dim / 2, 2] = magnitude (cos, sin)(position f_i), the
+ * angles in 64 bits, f_i = theta^(-2 i / rot_dim) before scaling for contexts longer than the model was trained on:
+ *   ATTS_ROTARY_PLAIN     f_i
+ *   ATTS_ROTARY_LINEAR    f_i / factor                                                        (positions interpolated)
+ *   ATTS_ROTARY_STRETCHED theta (factor^(rot_dim / (rot_dim - 2))) in place of theta           (rot_dim > 2)
+ *   ATTS_ROTARY_BY_PARTS  f_i (g + (1 - g) / factor), g = clamp((t_i - low) / (high - low), 0, 1) with t_i = original f_i / (2 pi) the turns of
+ *                         pair i within the original context: fast pairs stay, slow ones are interpolated
+ * theta > 0, factor > 0, magnitude and the rest finite, high > low, original > 0 (the last two for ATTS_ROTARY_BY_PARTS only). */
+#define ATTS_ROTARY_PLAIN     0
+#define ATTS_ROTARY_LINEAR    1
+#define ATTS_ROTARY_STRETCHED 2
+#define ATTS_ROTARY_BY_PARTS  3
+int32_t atts_rotary_table(int32_t scaling, double theta, int32_t rot_dim, double factor, double original, double low, double high,
+                          double magnitude, int64_t first, int64_t rows, float* table, void* hip_stream);
+
+/* Rotary embedding of the new rows' queries and keys, and their keys and values into the paged cache, in one launch.
+ *   qkv        dev [R, (n_q_heads + 2 n_kv_heads) head_dim] (dtype): q | k | v, rows qkv_stride elements apart, not modified
+ *   positions  dev int32 [R], read as clamped to [0, n_positions)
+ *   table      dev float [n_positions, rot_dim / 2, 2] (cos, sin), 8-byte aligned
+ *   layout     ATTS_ROTARY_HALF: element i of a head turns with element i + rot_dim / 2; ATTS_ROTARY_INTERLEAVED: 2 i with 2 i + 1
+ *              (i < rot_dim / 2); elements from rot_dim on stay as they are.  rot_dim even, 0 <= rot_dim <= head_dim
+ *   q_out      dev [R, n_q_heads head_dim] (dtype), contiguous
+ * The rotation is computed in 32 bits and rounded once.  Rows that no sequence owns are rotated and not stored.  Two rows must not share a
+ * cache slot. */
+#define ATTS_ROTARY_HALF        0
+#define ATTS_ROTARY_INTERLEAVED 1
+int32_t atts_rotary_append(const atts_paged_cache* cache, const void* qkv, int64_t qkv_stride, const int32_t* positions, const int32_t* cached,
+                           const int32_t* row_offsets, int32_t R, int32_t n_q_heads, const float* table, int32_t n_positions, int32_t rot_dim,
+                           int32_t layout, void* q_out, void* hip_stream);
+
+/* Attention of the new rows over the paged cache, which already holds their own keys and values (atts_rotary_append).  Row i of sequence s, at
+ * position cached[s] + depth(i) (its number of ancestors), attends to the tokens j < cached[s] at position j and to its
+ * ancestors and itself, of these to the ones whose position is less than `window` behind its own:
+ *   z = scale q . k;  softcap > 0: z = softcap tanh(z / softcap);  out = sum softmax(z) v
+ * Query head h reads key / value head h n_kv_heads / n_q_heads.
+ *   q, out      dev [R, n_q_heads head_dim] (dtype), 16-byte aligned (q)
+ *   max_rows    no sequence has more rows (later ones are left alone), <= ATTS_MAX_TREE;  max_cached: nor more cached tokens (further ones are not read)
+ *   scale       finite; softcap >= 0 (0: none); window >= 0 (0: none)
+ *   workspace   dev, 256-byte aligned, >= atts_attention_tree_workspace_bytes(...), scratch
+ * Keys and values that a row does not attend to, and slots behind a sequence's last row, never reach its output, NaN and infinities among them.
+ * Scores and sums are held in 32 bits; bf16: probabilities are rounded to 16 bits for their product with the values. */
+int32_t atts_attention_tree_workspace_bytes(const atts_paged_cache* cache, int32_t n_q_heads, int32_t R, int32_t max_rows, int32_t max_cached,
+                                            size_t* out_bytes);
+int32_t atts_attention_tree(const atts_paged_cache* cache, const void* q, const int32_t* parents, const int32_t* cached, const int32_t* row_offsets,
+                            int32_t R, int32_t n_q_heads, int32_t max_rows, int32_t max_cached, float scale, float softcap, int32_t window, void* out,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The logits of every new row under its request's rules, and what a decision needs of them, in one pass.  For token v of row r of sequence s,
+ * with params[s] = (repetition, frequency, presence, temperature), in 32 bits and in this order, each step rounded:
+ *   count      how often v was generated: history behind the first prompt_lens[s] entries, and on the row's own path in the tree
+ *              (the tree_ids of the row and of its ancestors)
+ *   1  x = x > 0 ? x / repetition : x repetition       if count > 0 or v is among the prompt's tokens
+ *   2  x = x - count frequency
+ *   3  x = x - presence                                if count > 0
+ *   4  x = x + bias                                    of several entries for one token the last one counts
+ *   5  x = x / temperature
+ *   6  x = -inf                                        if bit v % 32 of word v / 32 of the row's mask is 0
+ *   logits        dev [R, V] (dtype), rows logits_stride elements apart;  out the same with out_stride, may be the same array as logits
+ *   params        dev float [n_seqs, 4], or NULL: steps 1, 2, 3 and 5 are left out (and history, tree_ids are not read)
+ *   history       dev int32 [n_history], history_offsets dev int32 [n_seqs + 1], prompt_lens dev int32 [n_seqs] (NULL: 0); or all NULL
+ *   tree_ids, parents   dev int32 [R], or both NULL: rows have no path
+ *   bias_ids dev int32 [n_bias], bias_values dev float [n_bias], bias_offsets dev int32 [n_seqs + 1]; or all NULL
+ *   mask          dev uint32 [R, ceil(V / 32)], or NULL
+ *   top_ids       dev int32 [R] or NULL: the first arg max of the row's results before they are rounded to dtype, NaNs left out, -1 if none
+ *                 is above -inf;  lse dev float [R] or NULL: log sum exp of the same results (-inf if all are -inf)
+ *   workspace     dev, 256-byte aligned, >= atts_logits_adjust_workspace_bytes(R, V), scratch; may be NULL if top_ids and lse are
+ * Token ids outside [0, V) are ignored, offsets are read as clamped to their arrays.  max_rows <= ATTS_MAX_TREE as in atts_attention_tree.
+ * Rows that no sequence owns are left alone. */
+int32_t atts_logits_adjust_workspace_bytes(int32_t R, int32_t V, size_t* out_bytes);
+int32_t atts_logits_adjust(int32_t dtype, const void* logits, int64_t logits_stride, const int32_t* row_offsets, int32_t n_seqs, int32_t max_rows,
+                           const float* params, const int32_t* history, const int32_t* history_offsets, const int32_t* prompt_lens, int32_t n_history,
+                           const int32_t* tree_ids, const int32_t* parents, const int32_t* bias_ids, const float* bias_values,
+                           const int32_t* bias_offsets, int32_t n_bias, const uint32_t* mask, int32_t R, int32_t V, void* out, int64_t out_stride,
+                           int32_t* top_ids, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

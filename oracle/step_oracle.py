@@ -1,0 +1,130 @@
+"""One step over drafted token trees in plain numpy, 64 bits: products with 4-bit weights, rotary positions and the paged cache, attention of a
+tree, the logits' rules.  Written from the definitions in atts.h; nothing here is shared with the library."""
+import numpy as np
+
+
+# ---- 4-bit weights --------------------------------------------------------------------------------------------------
+
+def dequantize(codes, scales, zeros):
+    """codes uint8 [N, K / 2] -> [N, K]; zeros None: 8 everywhere"""
+    q = np.empty((codes.shape[0], 2 * codes.shape[1]))
+    q[:, 0::2], q[:, 1::2] = codes & 15, codes >> 4
+    group = q.shape[1] // scales.shape[1]
+    z = 8.0 if zeros is None else np.repeat(zeros.astype(np.float64), group, axis=1)
+    return (q - z) * np.repeat(scales.astype(np.float64), group, axis=1)
+
+
+def quant_product(x, codes, scales, zeros, epilogue, residual=None):
+    y = x.astype(np.float64) @ dequantize(codes, scales, zeros).T
+    if epilogue == "swiglu":
+        gate, up = np.split(y, 2, axis=1)
+        return gate / (1.0 + np.exp(-gate)) * up
+    return y + residual if epilogue == "residual" else y
+
+
+def quantize(w, group, symmetric, round_scale):
+    """codes [N, K], scales, zeros [N, K / group] by the rule of atts_quantize_rows in 32 bits; round_scale: to the type scales are stored in"""
+    g = w.astype(np.float32).reshape(w.shape[0], -1, group)
+    lo, hi = np.minimum(g.min(axis=2), np.float32(0)), np.maximum(g.max(axis=2), np.float32(0))
+    scale = round_scale(np.maximum(-lo / np.float32(8), hi / np.float32(7)) if symmetric else (hi - lo) / np.float32(15)).astype(np.float32)
+    safe = np.where(scale > 0, scale, np.float32(1))
+    zero = np.full_like(scale, 8) if symmetric else np.clip(np.rint(-lo / safe), 0, 15)
+    zero = np.where(scale > 0, zero, zero if symmetric else np.float32(0))
+    codes = np.where(scale[..., None] > 0, np.clip(np.rint(g / safe[..., None]) + zero[..., None], 0, 15), zero[..., None])
+    return codes.reshape(w.shape).astype(np.uint8), scale, zero.astype(np.uint8)
+
+
+# ---- rotary positions -----------------------------------------------------------------------------------------------
+
+def rotary_frequencies(theta, rot, scaling="plain", factor=1.0, original=0.0, low=0.0, high=0.0):
+    if scaling == "stretched":
+        theta = theta * factor ** (rot / (rot - 2))
+    f = theta ** (-2.0 * np.arange(rot // 2) / rot)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "by_parts":
+        g = np.clip((original * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+        f = f * (g + (1.0 - g) / factor)
+    return f
+
+
+def rotate(x, table_rows, interleaved):
+    """x [R, heads, hd], table_rows [R, rot / 2, 2]"""
+    x, rot = x.astype(np.float64), 2 * table_rows.shape[1]
+    y = x.copy()
+    c, s = table_rows[:, None, :, 0].astype(np.float64), table_rows[:, None, :, 1].astype(np.float64)
+    i = np.arange(rot // 2)
+    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+    y[..., a] = x[..., a] * c - x[..., b] * s
+    y[..., b] = x[..., b] * c + x[..., a] * s
+    return y
+
+
+# ---- trees and attention --------------------------------------------------------------------------------------------
+
+def path(parents, i):
+    """The row and its ancestors, the row first; an entry that is no earlier row ends the path."""
+    out = []
+    while i >= 0:
+        out.append(i)
+        up = int(parents[i])
+        i = up if 0 <= up < i else -1
+    return out
+
+
+def tree_attention(q, k, v, parents, cached, scale, softcap=0.0, window=0):
+    """One sequence: q [n, nq, hd], k / v [cached + n, nkv, hd].  Only the keys and values a row attends to are looked at."""
+    n, nq, hd = q.shape
+    out = np.empty((n, nq, hd))
+    for i in range(n):
+        own = path(parents, i)
+        keys = list(range(cached)) + [cached + t for t in sorted(own)]
+        at = np.array(list(range(cached)) + [cached + len(path(parents, t)) - 1 for t in sorted(own)])
+        keys = np.array(keys)
+        if window:
+            keys = keys[(cached + len(own) - 1) - at < window]
+        for h in range(nq):
+            g = h // (nq // k.shape[1])
+            z = scale * (k[keys, g].astype(np.float64) @ q[i, h].astype(np.float64))
+            if softcap:
+                z = softcap * np.tanh(z / softcap)
+            p = np.exp(z - z.max())
+            out[i, h] = (p / p.sum()) @ v[keys, g].astype(np.float64)
+    return out
+
+
+# ---- logits ---------------------------------------------------------------------------------------------------------
+
+def adjust(logits, params, prompt, generated, bias, mask_bits, dtype=np.float32):
+    """One row, every step rounded to dtype; params (repetition, frequency, presence, temperature) or None; bias: {token: value}; mask_bits bool [V]
+    or None.  -> results, index of the first arg max (-1: none above -inf)"""
+    f = dtype
+    x = logits.astype(f)
+    V = x.size
+    with np.errstate(all="ignore"):
+        if params is not None:
+            rep, freq, pres, temp = (f(p) for p in params)
+            inside = lambda ids: np.array([t for t in ids if 0 <= t < V], dtype=np.int64)
+            count = np.bincount(inside(generated), minlength=V)
+            known = count > 0
+            known[inside(prompt)] = True
+            x = np.where(known, np.where(x > 0, x / rep, x * rep), x)
+            x = x - count.astype(f) * freq
+            x = np.where(count > 0, x - pres, x)
+        for t, b in bias.items():
+            if 0 <= t < V:
+                x[t] = x[t] + f(b)
+        if params is not None:
+            x = x / temp
+        if mask_bits is not None:
+            x = np.where(mask_bits, x, f(-np.inf))
+    best = np.where(np.isnan(x), -np.inf, x)
+    return x, int(best.argmax()) if best.max() > -np.inf else -1
+
+
+def log_sum_exp(x):
+    x = x.astype(np.float64)
+    if np.isnan(x).any():
+        return np.nan
+    top = x.max()
+    return top if np.isinf(top) else top + np.log(np.exp(x - top).sum())

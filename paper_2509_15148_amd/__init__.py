@@ -18,6 +18,6 @@ def __getattr__(name):
         value = getattr(_BINDING, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
-    if name.startswith(("atts_", "Atts", "ERR_", "SCORE_")) or name in ("Model", "Prefix", "Calib"):
+    if name.startswith(("atts_", "Atts", "ERR_", "SCORE_", "EPILOGUE_", "ROTARY_")) or name in ("Model", "Prefix", "Calib", "PagedCache"):
         globals()[name] = value         # entry points are looked up on every call: found directly from now on
     return value

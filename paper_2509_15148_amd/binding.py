@@ -23,6 +23,10 @@ ERR_INVALID_ARG, ERR_SHAPE, ERR_WORKSPACE, ERR_CAPACITY, ERR_HIP = -1, -2, -3, -
 DTYPE_F32, DTYPE_BF16 = 0, 1
 SCORE_MEAN_NLL, SCORE_SUM_NLL = 0, 1
 MAX_ALPHAS = 8
+EPILOGUE_STORE, EPILOGUE_STORE_F32, EPILOGUE_RESIDUAL, EPILOGUE_SWIGLU = range(4)
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_STRETCHED, ROTARY_BY_PARTS = range(4)
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+MAX_TREE = 256
 
 # The C entry points and their arguments (p pointer, i int32_t, l int64_t, z size_t, f float, d double).  Declared once, they take
 # plain Python numbers and None: an argument object built for each of a short call's eleven arguments took longer than its kernels.
@@ -40,6 +44,10 @@ _ARGUMENTS = {
     "atts_classic_workspace_bytes": "lp", "atts_classic_normalize": "plipp", "atts_classic_threshold": "pldppzp",
     "atts_classic_prediction_sets": "plppp", "atts_gemm_routes": "iiiipp", "atts_pass_routes": "piiiiip", "atts_profile_enable": "i",
     "atts_profile_read": "ipp",
+    "atts_gemm_nt_quant": "iplpppippiiiip", "atts_quantize_rows": "ipiiipppp",
+    "atts_rotary_table": "ididddddllpp", "atts_rotary_append": "pplpppiipiiipp", "atts_attention_tree_workspace_bytes": "piiiip",
+    "atts_attention_tree": "pppppiiiiffippzp", "atts_logits_adjust_workspace_bytes": "iip",
+    "atts_logits_adjust": "iplpiippppipppppipiiplpppzp",
 }
 _C_TYPES = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "z": ctypes.c_size_t, "f": ctypes.c_float, "d": ctypes.c_double}
 EXPORTS = tuple(_ARGUMENTS)
@@ -481,6 +489,165 @@ def atts_classic_prediction_sets(scores: torch.Tensor, tau: torch.Tensor, member
         raise AttsError(ERR_INVALID_ARG, "member must have one element per score, tau one element")
     _check(_lib.atts_classic_prediction_sets(_ptr(scores, torch.float32, "scores"), scores.numel(),
                                              _ptr(tau, torch.float32, "tau"), _ptr(member, torch.uint8, "member"), _stream()))
+
+
+# ---- one step of the target model over drafted token trees --------------------------------------------------------
+
+def _rows(t: torch.Tensor, dtype, name: str):
+    """Address and row pitch of a matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise AttsError(ERR_INVALID_ARG, f"{name} must be a device tensor")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise AttsError(ERR_INVALID_ARG, f"{name} must be a matrix with contiguous rows")
+    if t.dtype != dtype:
+        raise AttsError(ERR_INVALID_ARG, f"{name} must have dtype {dtype}, got {t.dtype}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _count(t: Optional[torch.Tensor], n: int, name: str) -> None:
+    if t is not None and t.numel() != n:
+        raise AttsError(ERR_INVALID_ARG, f"{name} must have {n} elements, got {t.numel()}")
+
+
+def atts_gemm_nt_quant(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], out: torch.Tensor,
+                       epilogue: int = EPILOGUE_STORE, residual: Optional[torch.Tensor] = None) -> None:
+    """out = x W^T with W in 4-bit codes [rows, K / 2], scales and zeros [rows, K / group] (see atts.h for the epilogues)"""
+    if x.dim() != 2 or codes.dim() != 2 or scales.dim() != 2 or out.dim() != 2:
+        raise AttsError(ERR_INVALID_ARG, "x, codes, scales and out must be matrices")
+    (M, K), wide, groups = x.shape, codes.shape[0], scales.shape[1]
+    N = wide // 2 if epilogue == EPILOGUE_SWIGLU else wide
+    if codes.shape[1] * 2 != K or scales.shape[0] != wide or groups < 1 or K % groups or tuple(out.shape) != (M, N) or \
+            (epilogue == EPILOGUE_SWIGLU and wide % 2) or (zeros is not None and zeros.shape != scales.shape) or \
+            (epilogue == EPILOGUE_RESIDUAL and (residual is None or residual.shape != out.shape)):
+        raise AttsError(ERR_INVALID_ARG, "shape mismatch")
+    xp, ld = _rows(x, x.dtype, "x")
+    _check(_lib.atts_gemm_nt_quant(_dtype_code(x.dtype), xp, ld, _ptr(codes, torch.uint8, "codes"), _ptr(scales, x.dtype, "scales"),
+                                   _ptr(zeros, torch.uint8, "zeros"), K // groups,
+                                   _ptr(residual, torch.float32, "residual") if epilogue == EPILOGUE_RESIDUAL else None,
+                                   _ptr(out, torch.float32 if epilogue in (EPILOGUE_STORE_F32, EPILOGUE_RESIDUAL) else x.dtype, "out"),
+                                   M, N, K, ctypes.c_int32(epilogue), _stream()))
+
+
+def atts_quantize_rows(w: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None) -> None:
+    if w.dim() != 2 or codes.dim() != 2 or scales.dim() != 2:
+        raise AttsError(ERR_INVALID_ARG, "w, codes and scales must be matrices")
+    (N, K), groups = w.shape, scales.shape[1]
+    if tuple(codes.shape) != (N, K // 2) or scales.shape[0] != N or groups < 1 or K % groups or (zeros is not None and zeros.shape != scales.shape):
+        raise AttsError(ERR_INVALID_ARG, "shape mismatch")
+    _check(_lib.atts_quantize_rows(_dtype_code(w.dtype), _ptr(w, None, "w"), N, K, K // groups, _ptr(codes, torch.uint8, "codes"),
+                                   _ptr(scales, w.dtype, "scales"), _ptr(zeros, torch.uint8, "zeros"), _stream()))
+
+
+def atts_rotary_table(table: torch.Tensor, theta: float, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original: float = 0.0,
+                      low: float = 0.0, high: float = 0.0, magnitude: float = 1.0, first: int = 0) -> None:
+    """table [rows, rot_dim / 2, 2] for positions first .. first + rows - 1"""
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise AttsError(ERR_INVALID_ARG, "table must be [rows, rot_dim / 2, 2]")
+    _check(_lib.atts_rotary_table(ctypes.c_int32(scaling), ctypes.c_double(theta), 2 * table.shape[1], ctypes.c_double(factor),
+                                  ctypes.c_double(original), ctypes.c_double(low), ctypes.c_double(high), ctypes.c_double(magnitude),
+                                  ctypes.c_int64(first), table.shape[0], _ptr(table, torch.float32, "table"), _stream()))
+
+
+class _PagedDesc(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page_rows", "n_kv_heads", "head_dim", "n_seqs", "max_pages")]
+
+
+class PagedCache:
+    """A paged key / value cache over tensors that stay the caller's (kept alive, not copied): k_pages [n_pages, n_kv_heads, page_rows,
+    head_dim], v_pages [n_pages, n_kv_heads, head_dim, page_rows], page_table int32 [n_seqs, max_pages]."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor):
+        if k_pages.dim() != 4 or v_pages.dim() != 4 or page_table.dim() != 2 or \
+                tuple(v_pages.shape) != (k_pages.shape[0], k_pages.shape[1], k_pages.shape[3], k_pages.shape[2]):
+            raise AttsError(ERR_INVALID_ARG, "k_pages must be [pages, heads, page_rows, head_dim], v_pages [pages, heads, head_dim, page_rows], "
+                                             "page_table [n_seqs, max_pages]")
+        self.k_pages, self.v_pages, self.page_table, self.dtype = k_pages, v_pages, page_table, k_pages.dtype
+        self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k_pages.shape
+        self.n_seqs, self.max_pages = page_table.shape
+        self._desc = _PagedDesc(_ptr(k_pages, None, "k_pages"), _ptr(v_pages, k_pages.dtype, "v_pages"), _ptr(page_table, torch.int32, "page_table"),
+                                _dtype_code(k_pages.dtype), self.n_pages, self.page_rows, self.n_kv_heads, self.head_dim, self.n_seqs, self.max_pages)
+        self.handle = ctypes.addressof(self._desc)
+
+
+def atts_rotary_append(cache: PagedCache, qkv: torch.Tensor, positions: torch.Tensor, cached: torch.Tensor, row_offsets: torch.Tensor,
+                       table: torch.Tensor, layout: int, q_out: torch.Tensor) -> None:
+    if qkv.dim() != 2 or table.dim() != 3 or table.shape[2] != 2 or q_out.dim() != 2:
+        raise AttsError(ERR_INVALID_ARG, "qkv and q_out must be matrices, table [positions, rot_dim / 2, 2]")
+    R, hd = qkv.shape[0], cache.head_dim
+    n_q = qkv.shape[1] // hd - 2 * cache.n_kv_heads
+    if n_q < 0 or qkv.shape[1] != (n_q + 2 * cache.n_kv_heads) * hd or tuple(q_out.shape) != (R, n_q * hd):
+        raise AttsError(ERR_INVALID_ARG, "qkv must be [R, (n_q_heads + 2 n_kv_heads) head_dim], q_out [R, n_q_heads head_dim]")
+    _count(positions, R, "positions")
+    _count(cached, cache.n_seqs, "cached")
+    _count(row_offsets, cache.n_seqs + 1, "row_offsets")
+    ptr, ld = _rows(qkv, cache.dtype, "qkv")
+    _check(_lib.atts_rotary_append(cache.handle, ptr, ld, _ptr(positions, torch.int32, "positions"), _ptr(cached, torch.int32, "cached"),
+                                   _ptr(row_offsets, torch.int32, "row_offsets"), R, n_q, _ptr(table, torch.float32, "table"), table.shape[0],
+                                   2 * table.shape[1], ctypes.c_int32(layout), _ptr(q_out, cache.dtype, "q_out"), _stream()))
+
+
+def atts_attention_tree_workspace_bytes(cache: PagedCache, n_q_heads: int, R: int, max_rows: int, max_cached: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.atts_attention_tree_workspace_bytes(cache.handle, n_q_heads, R, max_rows, max_cached, ctypes.byref(out)))
+    return out.value
+
+
+def atts_attention_tree(cache: PagedCache, q: torch.Tensor, parents: torch.Tensor, cached: torch.Tensor, row_offsets: torch.Tensor, max_rows: int,
+                        max_cached: int, out: torch.Tensor, workspace: Optional[torch.Tensor], scale: Optional[float] = None,
+                        softcap: float = 0.0, window: int = 0) -> None:
+    """scale: 1 / sqrt(head_dim) unless given"""
+    if q.dim() != 2 or q.shape[1] % cache.head_dim or out.shape != q.shape:
+        raise AttsError(ERR_INVALID_ARG, "q and out must both be [R, n_q_heads head_dim]")
+    R = q.shape[0]
+    _count(parents, R, "parents")
+    _count(cached, cache.n_seqs, "cached")
+    _count(row_offsets, cache.n_seqs + 1, "row_offsets")
+    _check(_lib.atts_attention_tree(cache.handle, _ptr(q, cache.dtype, "q"), _ptr(parents, torch.int32, "parents"), _ptr(cached, torch.int32, "cached"),
+                                    _ptr(row_offsets, torch.int32, "row_offsets"), R, q.shape[1] // cache.head_dim, ctypes.c_int32(max_rows),
+                                    ctypes.c_int32(max_cached), ctypes.c_float(cache.head_dim ** -0.5 if scale is None else scale),
+                                    ctypes.c_float(softcap), ctypes.c_int32(window), _ptr(out, cache.dtype, "out"),
+                                    _ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()))
+
+
+def atts_logits_adjust_workspace_bytes(R: int, V: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.atts_logits_adjust_workspace_bytes(R, V, ctypes.byref(out)))
+    return out.value
+
+
+def atts_logits_adjust(logits: torch.Tensor, row_offsets: torch.Tensor, params: Optional[torch.Tensor], history: Optional[torch.Tensor],
+                       history_offsets: Optional[torch.Tensor], prompt_lens: Optional[torch.Tensor], tree_ids: Optional[torch.Tensor],
+                       parents: Optional[torch.Tensor], bias_ids: Optional[torch.Tensor], bias_values: Optional[torch.Tensor],
+                       bias_offsets: Optional[torch.Tensor], mask: Optional[torch.Tensor], out: torch.Tensor, top_ids: Optional[torch.Tensor],
+                       lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor], max_rows: Optional[int] = None) -> None:
+    """mask: int32 words of 32 bits, [R, ceil(V / 32)].  max_rows: the rows of the longest sequence (unless given, as many as there can be)"""
+    if logits.dim() != 2 or out.shape != logits.shape:
+        raise AttsError(ERR_INVALID_ARG, "logits and out must both be [R, V]")
+    (R, V), S = logits.shape, row_offsets.numel() - 1
+    if S < 0:
+        raise AttsError(ERR_INVALID_ARG, "row_offsets must have n_seqs + 1 elements")
+    if mask is not None and tuple(mask.shape) != (R, (V + 31) // 32):
+        raise AttsError(ERR_INVALID_ARG, "mask must be [R, ceil(V / 32)]")
+    for t, n, name in ((params, 4 * S, "params"), (history_offsets, S + 1, "history_offsets"), (prompt_lens, S, "prompt_lens"), (tree_ids, R, "tree_ids"),
+                       (parents, R, "parents"), (bias_offsets, S + 1, "bias_offsets"), (top_ids, R, "top_ids"), (lse, R, "lse")):
+        _count(t, n, name)
+    n_bias = 0 if bias_ids is None else bias_ids.numel()
+    _count(bias_values, n_bias, "bias_values")
+    if bias_ids is not None and bias_values is not None and n_bias == 0:       # an empty tensor has no address
+        bias_ids = bias_values = bias_offsets = None
+    if history is not None and history.numel() == 0 and history_offsets is not None:
+        history = history_offsets = prompt_lens = None
+    src, ld = _rows(logits, logits.dtype, "logits")
+    dst, out_ld = _rows(out, logits.dtype, "out")
+    _check(_lib.atts_logits_adjust(
+        _dtype_code(logits.dtype), src, ld, _ptr(row_offsets, torch.int32, "row_offsets"), S,
+        ctypes.c_int32(min(R, MAX_TREE) if max_rows is None else max_rows), _ptr(params, torch.float32, "params"),
+        _ptr(history, torch.int32, "history"), _ptr(history_offsets, torch.int32, "history_offsets"), _ptr(prompt_lens, torch.int32, "prompt_lens"),
+        0 if history is None else history.numel(), _ptr(tree_ids, torch.int32, "tree_ids"), _ptr(parents, torch.int32, "parents"),
+        _ptr(bias_ids, torch.int32, "bias_ids"), _ptr(bias_values, torch.float32, "bias_values"), _ptr(bias_offsets, torch.int32, "bias_offsets"),
+        n_bias, _ptr(mask, torch.int32, "mask"), R, V, dst, out_ld, _ptr(top_ids, torch.int32, "top_ids"), _ptr(lse, torch.float32, "lse"),
+        _ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()))
 
 
 def atts_gemm_routes(dtype: torch.dtype, M: int, N: int, Kdim: int):
