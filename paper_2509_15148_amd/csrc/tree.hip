@@ -1,88 +1,517 @@
 // Attention of drafted token trees over a paged key / value cache.
+//
+// For a sequence with L cached tokens and n new rows, group = n_q / n_kv query heads share a key / value head: its n group query rows all read
+// the same cached keys, and every row also reads the new rows it descends from.  A step reads each key and value once for a handful of
+// rows, so what bounds it is the cache's bytes: the kernel is built to keep loads in flight, straight from HBM into the registers that feed the matrix
+// cores, with no LDS and no barrier inside the loop.
+//
+//   * A wavefront holds up to 64 query rows (tiles of 16) and walks over tiles of 32 keys (16 in fp32).  S^T = K Q^T: the keys are the rows of the
+//     product, so lane (r = l % 16, c = l / 16) ends with scores of query row r only, of 8 (4) keys that lie one behind the other.  These are just
+//     the B operand of O^T = V^T P^T: the probabilities go from the accumulators into the next product without leaving their lane.
+//     Which key is which row of the first product is free, it is chosen so; the values are transposed in the cache, so their operand too is one
+//     16-byte load a lane.
+//   * The keys of the next tile are requested when the scores of this one are done, its values when they are used up: one set of registers, always
+//     one of the two under way.  Page numbers are read two tiles ahead.
+//   * exp2 with a reference that moves only when a score passes it by 8 (a probability is then at most 2^8): per tile one ballot instead of a
+//     reduction over lanes; sums stay in their lanes until the end.  bf16: probabilities are rounded to 16 bits for the second product, the
+//     matrix cores take nothing wider beside 16-bit values; their sum is of the unrounded ones.
+//   * Only tiles at a window's edge and those of the tree are masked.  There a lane checks its values: those that are not finite are taken out of the
+//     product (0 x NaN would reach every row) and added by themselves to the rows that see them.
+//   * The four wavefronts of a workgroup take every fourth tile and are joined through LDS; a long context is cut over workgroups
+//     (tree_plan), whose partial sums a second launch joins in their order.
 #include "paged.h"
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace atts {
 namespace {
 
+constexpr int kTreeWaves = 4;
+constexpr int kWords = ATTS_MAX_TREE / 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
 struct TreeArgs {
     const int32_t *parents, *cached, *row_offsets;
-    int32_t R, nq, max_rows, max_cached, window;
-    float scale, softcap;
+    float* part_o;               // [R n_q, max_splits, hd] sums of a split relative to its reference, [R n_q, max_splits] (reference, sum)
+    float2* part_ml;
+    int32_t R, nq, max_rows, max_cached, window, max_splits, tiles_per_split, row_tiles, n_groups;
+    float scale, softcap;        // scale: log2(e) scale, or without a cap's factor
 };
 
-// One wavefront per (row, query head): 64 keys at a time, a lane a key; then a lane holds elements lane, lane + 64, ... of the output.
-template <typename T>
-__global__ __launch_bounds__(64) void tree_rows_kernel(const T* __restrict__ q, const T* __restrict__ k_pages, const T* __restrict__ v_pages,
-                                                       T* __restrict__ out, PagedView p, TreeArgs a) {
-    const int lane = threadIdx.x, r = blockIdx.x, head = blockIdx.y, kv = head / (a.nq / p.n_kv), hd = p.hd;
-    const int seq = sequence_of(a.row_offsets, p.n_seqs, r);
-    if (seq < 0) return;
-    const int first = a.row_offsets[seq], own = r - first;
-    if (own >= a.max_rows || first < 0) return;
-    const int L = min(max(a.cached[seq], 0), min(a.max_cached, p.slots()));
-    __shared__ uint32_t mine[ATTS_MAX_TREE / 32];         // bit j: row j is the row itself or an ancestor
-    if (lane < ATTS_MAX_TREE / 32) mine[lane] = 0;
-    __syncthreads();
-    if (lane == 0)
-        for (int at = own; at >= 0;) {
-            mine[at >> 5] |= 1u << (at & 31);
-            const int parent = a.parents[first + at];
-            at = parent >= 0 && parent < at ? parent : -1;
-        }
-    __syncthreads();
-    int depth = -1;
-    for (int w = 0; w < ATTS_MAX_TREE / 32; ++w) depth += __popc(mine[w]);
-    const int here = L + depth;
-    const T* qr = q + ((int64_t)r * a.nq + head) * hd;
-    float m = -INFINITY, l = 0.f, acc[4] = {};
-    const int keys = min(L + own + 1, p.slots());
-    for (int j0 = 0; j0 < keys; j0 += 64) {
-        const int j = j0 + lane;
-        bool open = j < keys;
-        int at = j;
-        if (open && j >= L) {
-            const int t = j - L;
-            open = mine[t >> 5] >> (t & 31) & 1;
-            at = L - 1;
-            for (int w = 0; w <= t >> 5; ++w) at += __popc(w < t >> 5 ? mine[w] : mine[w] & (uint32_t)(2ull << (t & 31)) - 1);
-        }
-        if (a.window && here - at >= a.window) open = false;
-        float z = -INFINITY;
-        int page = 0;
-        if (open) {
-            page = p.page_of(seq, j);
-            if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
-            const T* kr = k_pages + p.key_at(page, kv, j);
-            z = 0.f;
-            for (int d = 0; d < hd; ++d) z += to_f32(qr[d]) * to_f32(kr[d]);
-            z *= a.scale;
-            if (a.softcap > 0.f) z = a.softcap * tanhf(z / a.softcap);
-        }
-        float top = z;
+// What a sequence is to its workgroups; every value is the same for all lanes.
+struct Sequence {
+    int first, n, L, lo, hi;     // first row, rows, cached tokens, first and last key any row may see (lo a multiple of 32)
+    __device__ Sequence(const PagedView& p, const TreeArgs& a, int seq) {
+        first = a.row_offsets[seq];
+        n = first < 0 ? 0 : max(0, min(min(a.row_offsets[seq + 1], a.R) - first, a.max_rows));
+        L = min(max(a.cached[seq], 0), min(a.max_cached, p.slots()));
+        lo = a.window ? max(0, L - a.window + 1) & ~31 : 0;
+        hi = min(L + n, p.slots());
+    }
+};
+
+template <typename T> struct Shape;
+template <> struct Shape<bf16> {
+    typedef bf16x8 Vec;                                   // 16 bytes
+    static constexpr int kKeys = 32, kLaneKeys = 8, kSub = 2, kStep = 32, kElems = 8;     // kStep: head elements a product step covers
+};
+template <> struct Shape<float> {
+    typedef f32x4 Vec;
+    static constexpr int kKeys = 16, kLaneKeys = 4, kSub = 1, kStep = 16, kElems = 4;
+};
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
 #pragma unroll
-        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-        const float next = fmaxf(m, top);
-        if (!(next > -INFINITY) && !__any(open)) continue;
-        const float keep = m > -INFINITY ? __expf(m - next) : 0.f;
-        const float e = open ? __expf(z - next) : 0.f;
-        float sum = e;
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// Over the four lanes l % 16 + 16 c of a query row.
+__device__ __forceinline__ float row_max(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool any_not_finite(bf16x8 v) {
+    const auto u = __builtin_bit_cast(uint4, v);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    bool bad = false;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        l = l * keep + sum;
-        m = next;
-        for (int i = 0; i < 4; ++i) acc[i] *= keep;
-        for (int t = 0; t < 64; ++t) {
-            if (!__shfl((int)open, t, 64)) continue;
-            const float w = __shfl(e, t, 64);
-            const T* vc = v_pages + p.value_at(__shfl(page, t, 64), kv, j0 + t);
-            for (int i = 0; i < 4; ++i)
-                if (lane + 64 * i < hd) acc[i] += w * to_f32(vc[(int64_t)(lane + 64 * i) << p.page_log]);
+    for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+__device__ __forceinline__ bool any_not_finite(f32x4 v) { return not_finite(v[0]) || not_finite(v[1]) || not_finite(v[2]) || not_finite(v[3]); }
+
+// HD: head_dim, or the next size up when EXACT is false; QT: tiles of 16 query rows.
+template <typename T, int HD, int QT, bool EXACT>
+__global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void tree_attention_kernel(
+        const T* __restrict__ q, const T* __restrict__ k_pages, const T* __restrict__ v_pages, T* __restrict__ out, PagedView p, TreeArgs a) {
+    using X = Shape<T>;
+    using Vec = typename X::Vec;
+    constexpr int kSteps = HD / X::kStep, kDims = HD / 16, kE = X::kLaneKeys, kRows = 16 * QT, kPitch = 36;
+    __shared__ uint32_t kin[ATTS_MAX_TREE][kWords];       // bit j of row i: row j is row i or an ancestor of it
+    __shared__ int16_t depth[ATTS_MAX_TREE];
+    __shared__ float2 ml[kTreeWaves][kRows];
+    __shared__ float sums[kTreeWaves][kRows][kPitch];
+
+    // Workgroups that read the same keys lie 8 apart, which is the same XCD and so the same L2.
+    const int id = blockIdx.x, row_tile = id / 8 % a.row_tiles, grp = id / (8 * a.row_tiles) * 8 + id % 8;
+    if (grp >= a.n_groups) return;
+    const int split = grp % a.max_splits, kv = grp / a.max_splits % p.n_kv, seq = grp / a.max_splits / p.n_kv;
+    const Sequence s(p, a, seq);
+    const int group = a.nq / p.n_kv, n_rows = s.n * group, hd = EXACT ? HD : p.hd;
+    const int tiles = max(1, (s.hi - s.lo + X::kKeys - 1) / X::kKeys);
+    const int tile0 = split * a.tiles_per_split, tile1 = min(tile0 + a.tiles_per_split, tiles);
+    if (row_tile * kRows >= n_rows || tile0 >= tile1) return;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, c = lane >> 4;
+    const bool tree_here = s.lo + tile1 * X::kKeys > s.L || a.window != 0;
+
+    Vec qf[QT][kSteps];
+    int own[QT];                                          // the row of the tree a query row belongs to
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int m = row_tile * kRows + t * 16 + r;
+        own[t] = min(m / group, s.n - 1);
+        const T* src = q + ((int64_t)(s.first + own[t]) * a.nq + kv * group + m % group) * hd;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int d = i * X::kStep + c * X::kElems;
+            qf[t][i] = m < n_rows && (EXACT || d < hd) ? *reinterpret_cast<const Vec*>(src + d) : Vec{};
         }
     }
-    for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < hd) out[((int64_t)r * a.nq + head) * hd + lane + 64 * i] = from_f32<T>(acc[i] / l);
+    if (tree_here) {
+        int up = -1;
+        if (tid < s.n) {
+            up = a.parents[s.first + tid];
+            if (up < 0 || up >= tid) up = -1;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) kin[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
+            depth[tid] = (int16_t)up;
+        }
+        __syncthreads();
+        // every round doubles the ancestors a row knows; depth holds how far up it has looked
+        for (int reach = 1; reach < s.n; reach *= 2) {
+            uint32_t more[kWords] = {};
+            int next = -1;
+            if (up >= 0) {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) more[w] = kin[up][w];
+                next = depth[up];
+            }
+            __syncthreads();
+            if (up >= 0) {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) kin[tid][w] |= more[w];
+                depth[tid] = (int16_t)next;
+            }
+            up = next;
+            __syncthreads();
+        }
+        if (tid < s.n) {
+            int above = -1;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) above += __popc(kin[tid][w]);
+            depth[tid] = (int16_t)above;
+        }
+        __syncthreads();
+    }
+    // tiles [open0, open1) are seen whole by every row: behind the last row's window, before the tree
+    const int open0 = a.window ? s.L + s.n - a.window : 0, open1 = s.L;
+
+    // Key rows of the first product: lane row r of sub-tile u is key 8 (r / 4) + 4 u + r % 4 (bf16), key r (fp32).
+    const int k_slot = X::kSub == 2 ? 8 * (r >> 2) + (r & 3) : r, v_slot = kE * c;
+    auto page_at = [&](int token) {
+        const int at = min(token >> p.page_log, p.max_pages - 1);
+        return p.table[(int64_t)seq * p.max_pages + at];
+    };
+    auto valid = [&](int page) { return (uint32_t)page < (uint32_t)p.n_pages ? page : 0; };
+    Vec kf[X::kSub][kSteps], vf[kDims];
+    auto load_keys = [&](int page, int key0) __attribute__((always_inline)) {
+        const T* src = k_pages + p.key_at(valid(page), kv, key0 + k_slot);
+#pragma unroll
+        for (int u = 0; u < X::kSub; ++u)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int d = i * X::kStep + c * X::kElems;
+                if (EXACT || d < hd) kf[u][i] = *reinterpret_cast<const Vec*>(src + u * 4 * hd + d);
+                else kf[u][i] = Vec{};
+            }
+    };
+    auto load_values = [&](int page, int key0) __attribute__((always_inline)) {
+        const T* src = v_pages + p.value_at(valid(page), kv, key0 + v_slot);
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) {
+            const int d = i * 16 + r;
+            vf[i] = *reinterpret_cast<const Vec*>(src + ((int64_t)(EXACT ? d : min(d, hd - 1)) << p.page_log));
+        }
+    };
+
+    f32x4 o[QT][kDims];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int my0 = tile0 + wave;
+    int key0 = s.lo + my0 * X::kKeys;
+    int pk = 0, pv = 0, pk_next = 0, pv_next = 0;         // pages of this and the next tile
+    if (my0 < tile1) {
+        pk = page_at(key0 + k_slot);
+        pv = page_at(key0 + v_slot);
+        pk_next = page_at(key0 + kTreeWaves * X::kKeys + k_slot);
+        pv_next = page_at(key0 + kTreeWaves * X::kKeys + v_slot);
+        load_keys(pk, key0);
+        load_values(pv, key0);
+    }
+    for (int tile = my0; tile < tile1; tile += kTreeWaves) {
+        const int next0 = key0 + kTreeWaves * X::kKeys;
+        const bool more = tile + kTreeWaves < tile1;
+        f32x4 z[QT][X::kSub];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int u = 0; u < X::kSub; ++u) {
+                z[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) z[t][u] = mma(kf[u][i], qf[t][i], z[t][u]);
+            }
+        const int pv_now = pv;
+        if (more) {
+            load_keys(pk_next, next0);
+            pk_next = page_at(next0 + kTreeWaves * X::kKeys + k_slot);
+        }
+
+        float e[QT][kE];
+        if (a.softcap > 0.f) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int j = 0; j < kE; ++j) {
+                    // cap tanh(x) with tanh x = 1 - 2 / (1 + exp 2x), in units of log2
+                    const float g = __builtin_amdgcn_exp2f(z[t][j >> 2][j & 3] * a.scale);
+                    e[t][j] = a.softcap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + g));
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int j = 0; j < kE; ++j) e[t][j] = z[t][j >> 2][j & 3] * a.scale;
+        }
+        const bool whole = key0 >= open0 && key0 + X::kKeys <= open1;
+        uint32_t open[QT];
+        if (!whole) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                open[t] = 0;
+#pragma unroll
+                for (int j = 0; j < kE; ++j) {
+                    const int key = key0 + v_slot + j, at = key - s.L;
+                    bool see = key < s.hi;
+                    int pos = key;
+                    if (see && at >= 0) {
+                        see = kin[own[t]][at >> 5] >> (at & 31) & 1;
+                        pos = s.L + depth[at];
+                    }
+                    if (see && a.window) see = s.L + depth[own[t]] - pos < a.window;
+                    open[t] |= (uint32_t)see << j;
+                    if (!see) e[t][j] = -INFINITY;
+                }
+            }
+        }
+        float top[QT];
+        bool move = false;
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            top[t] = e[t][0];
+#pragma unroll
+            for (int j = 1; j < kE; ++j) top[t] = fmaxf(top[t], e[t][j]);
+            move |= top[t] > m[t] + 8.f;
+        }
+        if (__builtin_amdgcn_ballot_w64(move) != 0) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const float ref = row_max(fmaxf(top[t], m[t]));
+                const float keep = ref == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - ref);
+                m[t] = ref;
+                l[t] *= keep;
+#pragma unroll
+                for (int i = 0; i < kDims; ++i) o[t][i] *= keep;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int j = 0; j < kE; ++j) {
+                e[t][j] = __builtin_amdgcn_exp2f(e[t][j] - m[t]);
+                if (!whole) e[t][j] = open[t] >> j & 1 ? e[t][j] : 0.f;
+                l[t] += e[t][j];
+            }
+        if (!whole) {
+            bool bad = false;
+            const int behind = min(max(s.hi - (key0 + v_slot), 0), kE);                   // keys that exist
+#pragma unroll
+            for (int i = 0; i < kDims; ++i) {
+#pragma unroll
+                for (int j = 0; j < kE; ++j) vf[i][j] = j < behind ? vf[i][j] : (T)0.f;
+                bad |= any_not_finite(vf[i]);
+            }
+            if (__builtin_amdgcn_ballot_w64(bad) != 0) {
+#pragma unroll
+                for (int i = 0; i < kDims; ++i)
+#pragma unroll
+                    for (int j = 0; j < kE; ++j) vf[i][j] = not_finite((float)vf[i][j]) ? (T)0.f : vf[i][j];
+#pragma unroll 1
+                for (int key = 0; key < X::kKeys; ++key) {
+                    if (key0 + key >= s.hi) break;
+                    const int from = key / kE, j = key % kE;
+                    const T* src = v_pages + p.value_at(valid(__shfl(pv_now, 16 * from, 64)), kv, key0 + key);
+                    float w[QT];
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        float mine = e[t][0];
+#pragma unroll
+                        for (int x = 1; x < kE; ++x) mine = x == j ? e[t][x] : mine;
+                        const bool sees = __shfl((int)open[t], r + 16 * from, 64) >> j & 1;
+                        mine = __shfl(mine, r + 16 * from, 64);
+                        w[t] = sees ? mine : -1.f;                                        // a probability is never negative
+                    }
+                    src += (int64_t)(4 * c) << p.page_log;
+#pragma unroll
+                    for (int i = 0; i < kDims; ++i) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const float v = EXACT || i * 16 + 4 * c + x < hd ? to_f32(*src) : 0.f;
+                            if (not_finite(v)) {
+#pragma unroll
+                                for (int t = 0; t < QT; ++t)
+                                    if (!(w[t] < 0.f)) o[t][i][x] += w[t] * v;
+                            }
+                            src += (int64_t)1 << p.page_log;
+                            asm volatile("" : "+v"(src));              // one address that moves on, not 4 kDims kept in registers
+                        }
+                        src += (int64_t)12 << p.page_log;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            Vec w;
+#pragma unroll
+            for (int j = 0; j < kE; ++j) w[j] = (T)e[t][j];
+#pragma unroll
+            for (int i = 0; i < kDims; ++i) o[t][i] = mma(vf[i], w, o[t][i]);
+        }
+        if (more) {
+            pv = pv_next;
+            load_values(pv, next0);
+            pv_next = page_at(next0 + kTreeWaves * X::kKeys + v_slot);
+        }
+        key0 = next0;
+    }
+
+    // The wavefronts together: references and sums first, then the outputs, 32 head elements at a time.
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        l[t] = row_sum(l[t]);
+        if (c == 0) ml[wave][t * 16 + r] = make_float2(m[t], l[t]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        float ref = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kTreeWaves; ++w) ref = fmaxf(ref, ml[w][t * 16 + r].x);
+        const float keep = m[t] == ref ? 1.f : __builtin_amdgcn_exp2f(m[t] - ref);
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) o[t][i] *= keep;
+    }
+    const bool alone = tiles <= a.tiles_per_split;
+    constexpr int kEach = kRows * 32 / (64 * kTreeWaves);           // elements a thread writes in a round
+    const int d_mine = tid & 31;
+#pragma unroll
+    for (int round = 0; round < kDims / 2; ++round) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r][i * 16 + 4 * c]) = o[t][round * 2 + i];
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) {
+            const int row = (tid >> 5) + x * (2 * kTreeWaves), mq = row_tile * kRows + row, d = round * 32 + d_mine;
+            if (mq >= n_rows || (!EXACT && d >= hd)) continue;
+            float ref = -INFINITY, sum = 0.f, y = 0.f;
+#pragma unroll
+            for (int w = 0; w < kTreeWaves; ++w) ref = fmaxf(ref, ml[w][row].x);
+#pragma unroll
+            for (int w = 0; w < kTreeWaves; ++w) {
+                const float2 one = ml[w][row];
+                sum += one.x == ref ? one.y : one.y * __builtin_amdgcn_exp2f(one.x - ref);
+                y += sums[w][row][d_mine];
+            }
+            const int64_t at = (int64_t)(s.first + mq / group) * a.nq + kv * group + mq % group;
+            if (alone) out[at * hd + d] = from_f32<T>(sum == 0.f ? 0.f : y / sum);
+            else {
+                a.part_o[(at * a.max_splits + split) * hd + d] = y;
+                if (d == 0) a.part_ml[at * a.max_splits + split] = make_float2(ref, sum);
+            }
+        }
+    }
+}
+
+// One workgroup per (row, query head) whose keys were cut: four wavefronts take every fourth split each, a lane up to four head elements.
+template <typename T>
+__global__ __launch_bounds__(256) void tree_join_kernel(T* __restrict__ out, PagedView p, TreeArgs a, int keys_per_tile) {
+    __shared__ float2 ml[4];
+    __shared__ float part[4][256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t at = blockIdx.x;
+    const int row = (int)(at / a.nq), seq = sequence_of(a.row_offsets, p.n_seqs, row);
+    if (seq < 0) return;
+    const Sequence s(p, a, seq);
+    if (row - s.first >= s.n) return;
+    const int tiles = max(1, (s.hi - s.lo + keys_per_tile - 1) / keys_per_tile);
+    if (tiles <= a.tiles_per_split) return;
+    const int splits = (tiles + a.tiles_per_split - 1) / a.tiles_per_split;
+    float ref = -INFINITY;
+    for (int i = lane; i < splits; i += 64) ref = fmaxf(ref, a.part_ml[at * a.max_splits + i].x);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d, 64));
+    float sum = 0.f, y[4] = {};
+#pragma unroll 4
+    for (int i = wave; i < splits; i += 4) {
+        const float2 one = a.part_ml[at * a.max_splits + i];
+        const float w = one.x == ref ? 1.f : __builtin_amdgcn_exp2f(one.x - ref);
+        sum += w * one.y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lane + 64 * j < p.hd) y[j] += w * a.part_o[(at * a.max_splits + i) * p.hd + lane + 64 * j];
+    }
+    if (lane == 0) ml[wave].y = sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][lane + 64 * j] = y[j];
+    __syncthreads();
+    const float total = ml[0].y + ml[1].y + ml[2].y + ml[3].y;
+    if (tid < p.hd) out[at * p.hd + tid] = from_f32<T>(total == 0.f ? 0.f : (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / total);
+}
+
+// How a call is cut: tiles of query rows, and splits of the longest sequence's keys.
+struct TreePlan {
+    int32_t q_tiles, row_tiles, tiles_per_split, max_splits;
+    size_t bytes;
+};
+
+constexpr int64_t kTreeWorkgroups = 512;                  // two a compute unit
+constexpr int64_t kTreePartRows = 1 << 16;                // (row, head, split) partial sums of a call that is cut
+
+TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max_rows, int32_t max_cached, int32_t window) {
+    TreePlan t{};
+    const int64_t rows = (int64_t)max_rows * (nq / c.n_kv_heads);
+    t.q_tiles = rows <= 16 ? 1 : rows <= 32 || c.head_dim > 128 ? 2 : 4;
+    t.row_tiles = (int32_t)std::max<int64_t>(1, ceil_div(rows, 16 * t.q_tiles));
+    const int64_t keys_per_tile = c.dtype == ATTS_DTYPE_F32 ? 16 : 32, slots = (int64_t)c.max_pages * c.page_rows;
+    const auto splits_of = [&](int64_t context) {         // 256 keys or more each
+        const int64_t keys = std::min(context + max_rows, slots);
+        return std::max<int64_t>(1, std::min(ceil_div(keys, 256), kTreePartRows / std::max<int64_t>(1, (int64_t)R * nq)));
+    };
+    // the bound of the workspace does not know the window, and grows with every argument
+    const int64_t bound = std::min((int64_t)R * nq * ceil_div(std::min((int64_t)max_cached + max_rows, slots), 256), kTreePartRows);
+    t.bytes = max_cached + max_rows <= 256 ? 0 : align_up((size_t)bound * (c.head_dim + 2) * sizeof(float), 256);
+    const int64_t context = window ? std::min((int64_t)max_cached, (int64_t)window + 31) : max_cached;
+    const int64_t cells = std::max<int64_t>(1, (int64_t)c.n_seqs * c.n_kv_heads * t.row_tiles);
+    const int64_t splits = std::min(splits_of(context), ceil_div(kTreeWorkgroups, cells));
+    const int64_t tiles = std::max<int64_t>(1, ceil_div(std::min(context + max_rows, slots), keys_per_tile));
+    t.tiles_per_split = (int32_t)ceil_div(tiles, splits);
+    t.max_splits = (int32_t)ceil_div(tiles, t.tiles_per_split);
+    return t;
+}
+
+template <typename T, int HD, int QT, bool EXACT>
+int32_t launch_tree(const atts_paged_cache& c, const void* q, void* out, const PagedView& p, const TreeArgs& a, hipStream_t stream) {
+    const int64_t wgs = ceil_div(a.n_groups, 8) * 8 * a.row_tiles;
+    if (wgs > 0x7fffffff) return fail(ATTS_ERR_SHAPE, "atts_attention_tree: the call has more than 2^31 workgroups");
+    hipLaunchKernelGGL((tree_attention_kernel<T, HD, QT, EXACT>), dim3((unsigned)wgs), dim3(64 * kTreeWaves), 0, stream, static_cast<const T*>(q),
+                       static_cast<const T*>(c.k_pages), static_cast<const T*>(c.v_pages), static_cast<T*>(out), p, a);
+    ATTS_LAUNCH_CHECK("tree_attention_kernel");
+    if (a.max_splits > 1) {
+        hipLaunchKernelGGL(tree_join_kernel<T>, dim3((unsigned)((int64_t)a.R * a.nq)), dim3(256), 0, stream, static_cast<T*>(out), p, a, Shape<T>::kKeys);
+        ATTS_LAUNCH_CHECK("tree_join_kernel");
+    }
+    return ATTS_OK;
+}
+
+template <typename T>
+int32_t launch_tree_shape(const TreePlan& t, const atts_paged_cache& c, const void* q, void* out, const PagedView& p, const TreeArgs& a, hipStream_t stream) {
+#define ATTS_TREE(HD, EXACT)                                                                         \
+    switch (t.q_tiles) {                                                                             \
+        case 1: return launch_tree<T, HD, 1, EXACT>(c, q, out, p, a, stream);                        \
+        case 2: return launch_tree<T, HD, 2, EXACT>(c, q, out, p, a, stream);                        \
+        default: return launch_tree<T, HD, (HD > 128 ? 2 : 4), EXACT>(c, q, out, p, a, stream);        \
+    }
+    if (p.hd == 64) { ATTS_TREE(64, true) }
+    if (p.hd == 128) { ATTS_TREE(128, true) }
+    if (p.hd == 256) { ATTS_TREE(256, true) }
+    if (p.hd < 128) { ATTS_TREE(128, false) }
+    ATTS_TREE(256, false)
+#undef ATTS_TREE
 }
 
 int32_t check_tree(const char* fn, const atts_paged_cache* cache, int32_t n_q_heads, int32_t R, int32_t max_rows, int32_t max_cached, PagedView* p) {
@@ -108,7 +537,7 @@ int32_t atts_attention_tree_workspace_bytes(const atts_paged_cache* cache, int32
     PagedView p;
     const int32_t rc = check_tree(fn, cache, n_q_heads, R, max_rows, max_cached, &p);
     if (rc != ATTS_OK) return rc;
-    *out_bytes = 0;
+    *out_bytes = tree_plan(*cache, n_q_heads, R, max_rows, max_cached, 0).bytes;
     return ATTS_OK;
 }
 
@@ -124,21 +553,20 @@ int32_t atts_attention_tree(const atts_paged_cache* cache, const void* q, const 
     if (R == 0 || p.n_seqs == 0 || max_rows == 0) return ATTS_OK;
     if (!q || !parents || !cached || !row_offsets || !out) return fail(ATTS_ERR_INVALID_ARG, "%s: NULL argument", fn);
     if ((uintptr_t)q & 15) return fail(ATTS_ERR_INVALID_ARG, "%s: q must be 16-byte aligned", fn);
-    size_t need = 0;
-    rc = atts_attention_tree_workspace_bytes(cache, n_q_heads, R, max_rows, max_cached, &need);
-    if (rc != ATTS_OK) return rc;
-    if (need && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need))
-        return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, need);
-    const TreeArgs a{parents, cached, row_offsets, R, n_q_heads, max_rows, max_cached, window, scale, softcap};
+    const TreePlan t = tree_plan(*cache, n_q_heads, R, max_rows, max_cached, window);
+    if (t.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < t.bytes))
+        return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, t.bytes);
+    const int64_t groups = (int64_t)p.n_seqs * p.n_kv * t.max_splits;
+    if (groups > (1 << 30)) return fail(ATTS_ERR_SHAPE, "%s: the call has more than 2^30 groups of workgroups", fn);
+    float* part_o = static_cast<float*>(workspace);
+    float2* part_ml = reinterpret_cast<float2*>(part_o + (int64_t)R * n_q_heads * t.max_splits * p.hd);
+    // with a cap, scores enter tanh as 2 log2(e) scale / cap, and leave it in units of log2
+    const float in = softcap > 0.f ? 2.f * kLog2e * scale / softcap : kLog2e * scale;
+    const TreeArgs a{parents, cached, row_offsets, part_o, part_ml, R, n_q_heads, max_rows, max_cached, window, t.max_splits, t.tiles_per_split,
+                     t.row_tiles, (int32_t)groups, in, softcap * kLog2e};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (cache->dtype == ATTS_DTYPE_F32)
-        hipLaunchKernelGGL(tree_rows_kernel<float>, dim3((unsigned)R, (unsigned)n_q_heads), dim3(64), 0, stream, static_cast<const float*>(q),
-                           static_cast<const float*>(cache->k_pages), static_cast<const float*>(cache->v_pages), static_cast<float*>(out), p, a);
-    else
-        hipLaunchKernelGGL(tree_rows_kernel<bf16>, dim3((unsigned)R, (unsigned)n_q_heads), dim3(64), 0, stream, static_cast<const bf16*>(q),
-                           static_cast<const bf16*>(cache->k_pages), static_cast<const bf16*>(cache->v_pages), static_cast<bf16*>(out), p, a);
-    ATTS_LAUNCH_CHECK("tree_rows_kernel");
-    return ATTS_OK;
+    if (cache->dtype == ATTS_DTYPE_F32) return launch_tree_shape<float>(t, *cache, q, out, p, a, stream);
+    return launch_tree_shape<bf16>(t, *cache, q, out, p, a, stream);
 }
 
 }  // extern "C"
