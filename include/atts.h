@@ -466,19 +466,21 @@ typedef struct {
  *   x         dev [M, Kdim] (dtype), rows x_stride elements apart, 16-byte aligned, x_stride * sizeof(dtype) a multiple of 16
  *   codes     dev uint8 [rows, Kdim / 2], 16-byte aligned: code k of a row is the low (k even) or high half of byte k / 2
  *   scales    dev [rows, Kdim / group] (dtype);  zeros dev uint8 [rows, Kdim / group], or NULL: 8 everywhere
- *   group     32, 64 or 128; divides Kdim
+ *   group     32, 64 or 128; divides Kdim, which is at most 2^24 (and x_stride 2^25)
  *   epilogue  ATTS_EPILOGUE_STORE      out (dtype) [M, N] = product                         (rows of W: N)
  *             ATTS_EPILOGUE_STORE_F32  out (float) [M, N] = product
  *             ATTS_EPILOGUE_RESIDUAL   out (float) [M, N] = residual + product; residual dev float [M, N], out may be the same array
  *             ATTS_EPILOGUE_SWIGLU     out (dtype) [M, N] = silu(gate) * up                 (rows of W: N gate rows, then N up rows)
- * M >= 0 (0 is a no-op), N >= 1.  Meant for up to about a hundred rows: the weights are read once for every 64. */
+ * M >= 0 (0 is a no-op), N >= 1.  Meant for up to about a hundred rows.  A row of X that is not finite gives a row that is not.
+ *   workspace dev, 256-byte aligned, >= atts_gemm_nt_quant_workspace_bytes(...), scratch; may be NULL where that is 0 */
 #define ATTS_EPILOGUE_STORE     0
 #define ATTS_EPILOGUE_STORE_F32 1
 #define ATTS_EPILOGUE_RESIDUAL  2
 #define ATTS_EPILOGUE_SWIGLU    3
+int32_t atts_gemm_nt_quant_workspace_bytes(int32_t dtype, int32_t M, int32_t N, int32_t Kdim, int32_t epilogue, size_t* out_bytes);
 int32_t atts_gemm_nt_quant(int32_t dtype, const void* x, int64_t x_stride, const uint8_t* codes, const void* scales, const uint8_t* zeros,
                            int32_t group, const float* residual, void* out, int32_t M, int32_t N, int32_t Kdim, int32_t epilogue,
-                           void* hip_stream);
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Codes, scales and zeros of a matrix w dev [N, Kdim] (dtype) for atts_gemm_nt_quant, group by group.  With lo = min(0, smallest) and hi =
  * max(0, largest) value of the group:

@@ -44,7 +44,7 @@ _ARGUMENTS = {
     "atts_classic_workspace_bytes": "lp", "atts_classic_normalize": "plipp", "atts_classic_threshold": "pldppzp",
     "atts_classic_prediction_sets": "plppp", "atts_gemm_routes": "iiiipp", "atts_pass_routes": "piiiiip", "atts_profile_enable": "i",
     "atts_profile_read": "ipp",
-    "atts_gemm_nt_quant": "iplpppippiiiip", "atts_quantize_rows": "ipiiipppp",
+    "atts_gemm_nt_quant_workspace_bytes": "iiiiip", "atts_gemm_nt_quant": "iplpppippiiiipzp", "atts_quantize_rows": "ipiiipppp",
     "atts_rotary_table": "ididddddllpp", "atts_rotary_append": "pplpppiipiiipp", "atts_attention_tree_workspace_bytes": "piiiip",
     "atts_attention_tree": "pppppiiiiffippzp", "atts_logits_adjust_workspace_bytes": "iip",
     "atts_logits_adjust": "iplpiippppipppppipiiplpppzp",
@@ -509,9 +509,16 @@ def _count(t: Optional[torch.Tensor], n: int, name: str) -> None:
         raise AttsError(ERR_INVALID_ARG, f"{name} must have {n} elements, got {t.numel()}")
 
 
+def atts_gemm_nt_quant_workspace_bytes(dtype: torch.dtype, M: int, N: int, K: int, epilogue: int = EPILOGUE_STORE) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.atts_gemm_nt_quant_workspace_bytes(_dtype_code(dtype), M, N, K, epilogue, ctypes.byref(out)))
+    return out.value
+
+
 def atts_gemm_nt_quant(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], out: torch.Tensor,
-                       epilogue: int = EPILOGUE_STORE, residual: Optional[torch.Tensor] = None) -> None:
-    """out = x W^T with W in 4-bit codes [rows, K / 2], scales and zeros [rows, K / group] (see atts.h for the epilogues)"""
+                       epilogue: int = EPILOGUE_STORE, residual: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """out = x W^T with W in 4-bit codes [rows, K / 2], scales and zeros [rows, K / group] (see atts.h for the epilogues).  Without a workspace, a
+    call that needs one takes it from torch's allocator for its own duration on the current stream."""
     if x.dim() != 2 or codes.dim() != 2 or scales.dim() != 2 or out.dim() != 2:
         raise AttsError(ERR_INVALID_ARG, "x, codes, scales and out must be matrices")
     (M, K), wide, groups = x.shape, codes.shape[0], scales.shape[1]
@@ -521,11 +528,15 @@ def atts_gemm_nt_quant(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
             (epilogue == EPILOGUE_RESIDUAL and (residual is None or residual.shape != out.shape)):
         raise AttsError(ERR_INVALID_ARG, "shape mismatch")
     xp, ld = _rows(x, x.dtype, "x")
+    if workspace is None and M > 16:                    # up to 16 rows nothing is cut
+        need = atts_gemm_nt_quant_workspace_bytes(x.dtype, M, N, K, epilogue)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _check(_lib.atts_gemm_nt_quant(_dtype_code(x.dtype), xp, ld, _ptr(codes, torch.uint8, "codes"), _ptr(scales, x.dtype, "scales"),
                                    _ptr(zeros, torch.uint8, "zeros"), K // groups,
                                    _ptr(residual, torch.float32, "residual") if epilogue == EPILOGUE_RESIDUAL else None,
                                    _ptr(out, torch.float32 if epilogue in (EPILOGUE_STORE_F32, EPILOGUE_RESIDUAL) else x.dtype, "out"),
-                                   M, N, K, ctypes.c_int32(epilogue), _stream()))
+                                   M, N, K, ctypes.c_int32(epilogue), _ptr(workspace, torch.uint8, "workspace"),
+                                   0 if workspace is None else workspace.numel(), _stream()))
 
 
 def atts_quantize_rows(w: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None) -> None:

@@ -11,78 +11,300 @@ struct QuantArgs {
     const uint8_t* zeros;
     const float* residual;
     void* out;
+    float* parts;                // K cut over workgroups: their sums, [splits][M][rows of W]
     int64_t x_stride;
-    int32_t M, N, K, group_log, groups;
+    int32_t M, N, K, groups, epilogue, wide;      // wide: rows of W
+    int32_t splits, steps_per_split, steps, row_blocks, tiles;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
-template <typename T, int EPI>
-__device__ __forceinline__ void store(const QuantArgs& a, int m, int n, float y) {
-    const int64_t at = (int64_t)m * a.N + n;
-    if constexpr (EPI == ATTS_EPILOGUE_RESIDUAL) reinterpret_cast<float*>(a.out)[at] = a.residual[at] + y;
-    else if constexpr (EPI == ATTS_EPILOGUE_STORE_F32) reinterpret_cast<float*>(a.out)[at] = y;
-    else reinterpret_cast<T*>(a.out)[at] = from_f32<T>(y);
-}
+constexpr int kQuantWaves = 8;
+constexpr int kSpan = 128;       // K elements of a step: 16 bytes of codes a lane
 
 __device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
 
-// One wavefront per output feature: lane l takes eight codes at a time, 4 rows of X in one sweep.
-template <typename T, int EPI>
-__global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a) {
-    constexpr int kRows = 4, kWide = EPI == ATTS_EPILOGUE_SWIGLU ? 2 : 1;
-    const int lane = threadIdx.x & 63;
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (n >= a.N) return;
-    const T* x = reinterpret_cast<const T*>(a.x);
-    const T* scales = reinterpret_cast<const T*>(a.scales);
-    for (int m0 = 0; m0 < a.M; m0 += kRows) {
-        float acc[kWide][kRows] = {};
-        for (int w = 0; w < kWide; ++w) {
-            const int64_t row = n + (int64_t)w * a.N;
-            for (int k = lane * 8; k < a.K; k += 512) {
-                const uint32_t word = *reinterpret_cast<const uint32_t*>(a.codes + row * (a.K / 2) + k / 2);
-                const int64_t g = row * a.groups + (k >> a.group_log);
-                const float scale = to_f32(scales[g]);
-                const float zero = a.zeros ? (float)a.zeros[g] : 8.f;
+template <typename T>
+__device__ __forceinline__ void finish(const QuantArgs& a, int m, int n, float y, float up) {
+    const int64_t at = (int64_t)m * a.N + n;
+    if (a.epilogue == ATTS_EPILOGUE_RESIDUAL) reinterpret_cast<float*>(a.out)[at] = a.residual[at] + y;
+    else if (a.epilogue == ATTS_EPILOGUE_STORE_F32) reinterpret_cast<float*>(a.out)[at] = y;
+    else reinterpret_cast<T*>(a.out)[at] = from_f32<T>(a.epilogue == ATTS_EPILOGUE_SWIGLU ? silu(y) * up : y);
+}
+
+// Eight activations as they meet the codes of a word: 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ bf16x8 in_code_order(const uint4& d) {
+    uint4 o;
+    o.x = __builtin_amdgcn_perm(d.z, d.x, 0x05040100u);
+    o.y = __builtin_amdgcn_perm(d.z, d.x, 0x07060302u);
+    o.z = __builtin_amdgcn_perm(d.w, d.y, 0x05040100u);
+    o.w = __builtin_amdgcn_perm(d.w, d.y, 0x07060302u);
+    return __builtin_bit_cast(bf16x8, o);
+}
+
+// What the matrix cores take of eight activations: themselves, or three 16-bit parts whose sum is the 32-bit value.
+template <typename T> struct Parts;
+template <> struct Parts<bf16> {
+    static constexpr int kN = 1, kLoads = 1;
+    bf16x8 v[1];
+    __device__ explicit Parts(const uint4* raw) { v[0] = in_code_order(raw[0]); }
+};
+template <> struct Parts<float> {
+    static constexpr int kN = 3, kLoads = 2;
+    bf16x8 v[3];
+    __device__ explicit Parts(const uint4* raw) {
+        const f32x4 lo = __builtin_bit_cast(f32x4, raw[0]), hi = __builtin_bit_cast(f32x4, raw[1]);
 #pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                    const T* xr = x + (int64_t)min(m0 + r, a.M - 1) * a.x_stride + k;
-                    float s = 0.f;
+        for (int i = 0; i < 8; ++i) {
+            float x = i & 1 ? hi[i >> 1] : lo[i >> 1];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s += ((float)((word >> (4 * j)) & 15) - zero) * to_f32(xr[j]);
-                    acc[w][r] += scale * s;
+            for (int part = 0; part < 3; ++part) {
+                v[part][i] = (bf16)x;
+                x -= (float)v[part][i];
+            }
+        }
+    }
+};
+
+// Eight codes as 16 + code, exact in 16 bits: the code goes to the upper four of the seven stored bits of 16 = 0x4180.
+__device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
+    uint4 o;
+    o.x = (w << 3 & 0x00780078u) | 0x41804180u;
+    o.y = (w >> 1 & 0x00780078u) | 0x41804180u;
+    o.z = (w >> 5 & 0x00780078u) | 0x41804180u;
+    o.w = (w >> 9 & 0x00780078u) | 0x41804180u;
+    return __builtin_bit_cast(bf16x8, o);
+}
+
+// Word j of quarter-wave c for word c of quarter-wave j.
+__device__ __forceinline__ void swap_quarters(uint4& w) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w.x, w.z, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(w.y, w.w, false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    w = make_uint4(c[0], c[1], d[0], d[1]);
+}
+
+// A workgroup: NS blocks of 16 weight rows (SwiGLU: gate and up blocks in turn) times MT blocks of 16 rows of X, over one split of K; its wavefronts
+// take every eighth step.  G: group size.
+template <typename T, int G, int NS, int MT>
+__global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a) {
+    using P = Parts<T>;
+    constexpr int kGroups = kSpan / G, kRows = 16 * MT, kCols = 16 * NS, kPitch = kCols + 4;
+    __shared__ float red[kQuantWaves][16][kPitch];
+    // Workgroups of the same weights and other rows of X lie 8 apart: the same XCD, and so the same L2.
+    const int id = blockIdx.x, row_block = id / 8 % a.row_blocks, cell = id / (8 * a.row_blocks) * 8 + id % 8;
+    if (cell >= a.tiles * a.splits) return;
+    const int tile = cell % a.tiles, split = cell / a.tiles;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, c = lane >> 4;
+    const bool swiglu = a.epilogue == ATTS_EPILOGUE_SWIGLU;
+    const int m0 = row_block * kRows, t0 = split * a.steps_per_split + wave, t1 = min((split + 1) * a.steps_per_split, a.steps);
+
+    // Every address is a base that the whole workgroup shares and an offset of 32 bits.  Block s begins at weight row first[s]; rows past the
+    // last one are read as it, here and in X, and dropped at the end.
+    int64_t first[NS];
+    uint32_t row[NS], x_at[MT];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int n = swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16;
+        const int in = max(0, min(n, a.N - 1));                             // the block itself may lie behind the end
+        first[s] = in + (swiglu ? (int64_t)(s & 1) * a.N : 0);
+        row[s] = (uint32_t)min(r, a.N - 1 - in);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x_at[m] = (uint32_t)(min(m * 16 + r, a.M - 1 - m0) * a.x_stride + c * 8) * sizeof(T);
+    const char* const x0 = reinterpret_cast<const char*>(a.x) + m0 * a.x_stride * (int64_t)sizeof(T);
+
+    struct Step {
+        uint4 w[NS], x[MT][4][P::kLoads];
+        struct { T v[kGroups]; } scale[NS];
+        struct { uint8_t v[kGroups]; } zero[NS];
+    };
+    auto load = [&](Step& f, int t) __attribute__((always_inline)) {
+        const int k = min(t, t1 - 1) * kSpan;                               // past the end: a repeat, not used
+        const uint32_t mine = k + c * 32 < a.K ? c * 16 : 0;                // a last step may be partly filled
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+            f.w[s] = *reinterpret_cast<const uint4*>(a.codes + first[s] * (a.K / 2) + k / 2 + (row[s] * (uint32_t)(a.K / 2) + mine));
+        const T* scales = reinterpret_cast<const T*>(a.scales) + k / G;
+        if (k + kSpan <= a.K) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const uint32_t at = row[s] * (uint32_t)a.groups;
+                __builtin_memcpy(&f.scale[s], scales + first[s] * a.groups + at, sizeof(f.scale[s]));
+                if (a.zeros) __builtin_memcpy(&f.zero[s], a.zeros + first[s] * a.groups + k / G + at, sizeof(f.zero[s]));
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const uint32_t at = row[s] * (uint32_t)a.groups + min(g, a.groups - 1 - k / G);
+                    f.scale[s].v[g] = scales[first[s] * a.groups + at];
+                    if (a.zeros) f.zero[s].v[g] = a.zeros[first[s] * a.groups + k / G + at];
+                }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < P::kLoads; ++i)
+                    f.x[m][j][i] = *reinterpret_cast<const uint4*>(x0 + (int64_t)(k + (k + j * 32 < a.K ? j * 32 : 0)) * sizeof(T) + i * 16 + x_at[m]);
+    };
+    f32x4 acc[NS][MT];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[s][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+    auto use = [&](Step& f, int t) __attribute__((always_inline)) {
+        if (t >= t1) return;                                                // wave-uniform
+        f32x4 sum[NS][MT], sx[MT];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) swap_quarters(f.w[s]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j > 0 && t * kSpan + j * 32 >= a.K) break;                  // wave-uniform
+            if (j * 32 % G == 0) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    sx[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) sum[s][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+            }
+            bf16x8 w[NS];
+#pragma unroll
+            for (int s = 0; s < NS; ++s) w[s] = codes_plus_16(j == 0 ? f.w[s].x : j == 1 ? f.w[s].y : j == 2 ? f.w[s].z : f.w[s].w);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const P part(f.x[m][j]);
+#pragma unroll
+                for (int i = 0; i < P::kN; ++i) {
+                    sx[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part.v[i], ones, sx[m], 0, 0, 0);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) sum[s][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part.v[i], w[s], sum[s][m], 0, 0, 0);
+                }
+            }
+            if ((j + 1) * 32 % G == 0) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const float scale = to_f32(f.scale[s].v[j * 32 / G]), zero = a.zeros ? 16.f + (float)f.zero[s].v[j * 32 / G] : 24.f;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[s][m][i] = fmaf(scale, fmaf(-zero, sx[m][i], sum[s][m][i]), acc[s][m][i]);
                 }
             }
         }
+    };
+
+    Step fa, fb;
+    if (t0 < t1) {
+        load(fa, t0);
+        load(fb, t0 + kQuantWaves);
+        for (int t = t0; t < t1; t += 2 * kQuantWaves) {
+            use(fa, t);
+            load(fa, t + 2 * kQuantWaves);
+            use(fb, t + kQuantWaves);
+            load(fb, t + 3 * kQuantWaves);
+        }
+    }
+
+    // acc[s][m][i]: row 4 c + i of block m, column r of block s.  The wavefronts' sums are added in their order.
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            float y = wave_sum(acc[0][r]);
-            if constexpr (EPI == ATTS_EPILOGUE_SWIGLU) y = silu(y) * wave_sum(acc[kWide - 1][r]);
-            if (lane == 0 && m0 + r < a.M) store<T, EPI>(a, m0 + r, n, y);
+    for (int m = 0; m < MT; ++m) {
+        if (m) __syncthreads();
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][4 * c + i][s * 16 + r] = acc[s][m][i];
+        __syncthreads();
+        const int outs = swiglu && a.splits == 1 ? kCols / 2 : kCols;
+        for (int e = tid; e < 16 * outs; e += 64 * kQuantWaves) {
+            const int row = e / outs, o = e - row * outs, mrow = m0 + m * 16 + row;
+            if (mrow >= a.M) continue;
+            auto total = [&](int col) {
+                float y = 0.f;
+#pragma unroll
+                for (int w = 0; w < kQuantWaves; ++w) y += red[w][row][col];
+                return y;
+            };
+            if (a.splits > 1) {
+                const int n = swiglu ? tile * (kCols / 2) + o / 32 * 16 + o % 16 : tile * kCols + o;
+                if (n < a.N) a.parts[((int64_t)split * a.M + mrow) * a.wide + n + (swiglu ? (o / 16 & 1) * a.N : 0)] = total(o);
+            } else if (swiglu) {
+                const int n = tile * (kCols / 2) + o, col = o / 16 * 32 + o % 16;
+                if (n < a.N) finish<T>(a, mrow, n, total(col), total(col + 16));
+            } else if (tile * kCols + o < a.N) finish<T>(a, mrow, tile * kCols + o, total(o), 0.f);
         }
     }
 }
 
-template <typename T, int EPI>
-int32_t launch_quant(const QuantArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((quant_rows_kernel<T, EPI>), dim3((unsigned)ceil_div(a.N, 4)), dim3(256), 0, stream, a);
-    ATTS_LAUNCH_CHECK("quant_rows_kernel");
+// The splits' sums of one element, in their order, and the epilogue.
+template <typename T>
+__global__ __launch_bounds__(256) void quant_join_kernel(QuantArgs a) {
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= (int64_t)a.M * a.N) return;
+    const int m = (int)(e / a.N), n = (int)(e - (int64_t)m * a.N);
+    const int64_t pitch = (int64_t)a.M * a.wide;
+    const float* src = a.parts + (int64_t)m * a.wide + n;
+    float y = 0.f, up = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        y += src[s * pitch];
+        if (a.epilogue == ATTS_EPILOGUE_SWIGLU) up += src[s * pitch + a.N];
+    }
+    finish<T>(a, m, n, y, up);
+}
+
+// How a call is cut.
+struct QuantPlan {
+    int32_t ns, mt, tiles, splits, steps, steps_per_split, row_blocks;
+    size_t bytes;
+};
+
+QuantPlan quant_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t epilogue) {
+    constexpr int64_t kChip = 256;                         // compute units
+    QuantPlan p{};
+    const int64_t wide = epilogue == ATTS_EPILOGUE_SWIGLU ? 2 * (int64_t)N : N;
+    p.mt = M <= 16 || dtype == ATTS_DTYPE_F32 ? 1 : 2;     // fp32: three parts of X and their sums leave no room for a second block
+    p.row_blocks = (int32_t)ceil_div(M, 16 * p.mt);
+    p.ns = M > 16 || ceil_div(wide, 64) >= kChip ? 4 : epilogue == ATTS_EPILOGUE_SWIGLU || ceil_div(wide, 32) >= kChip ? 2 : 1;
+    const int64_t tiles = ceil_div(wide, 16 * p.ns);
+    p.tiles = (int32_t)(epilogue == ATTS_EPILOGUE_SWIGLU ? ceil_div(N, 8 * p.ns) : tiles);
+    p.steps = (int32_t)ceil_div(K, kSpan);
+    int64_t splits = 1;
+    if (M > 16) {
+        splits = kChip / ((int64_t)p.tiles * p.row_blocks);
+        const int64_t most = p.steps / (2 * kQuantWaves);     // two steps a wavefront at least
+        if (splits > most) splits = most;
+        if (splits < 1) splits = 1;
+    }
+    p.steps_per_split = (int32_t)ceil_div(p.steps, splits);
+    p.splits = (int32_t)ceil_div(p.steps, p.steps_per_split);
+    p.bytes = p.splits > 1 ? (size_t)p.splits * M * wide * sizeof(float) : 0;
+    return p;
+}
+
+template <typename T, int G>
+int32_t launch_quant(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
+    const int64_t wgs = ceil_div((int64_t)p.tiles * p.splits, 8) * 8 * p.row_blocks;
+    if (wgs > 0x7fffffff) return fail(ATTS_ERR_SHAPE, "atts_gemm_nt_quant: the call has more than 2^31 workgroups");
+    const dim3 grid((unsigned)wgs), block(64 * kQuantWaves);
+    if (p.mt == 2) hipLaunchKernelGGL((quant_kernel<T, G, 4, sizeof(T) == 2 ? 2 : 1>), grid, block, 0, stream, a);
+    else if (p.ns == 4) hipLaunchKernelGGL((quant_kernel<T, G, 4, 1>), grid, block, 0, stream, a);
+    else if (p.ns == 2) hipLaunchKernelGGL((quant_kernel<T, G, 2, 1>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((quant_kernel<T, G, 1, 1>), grid, block, 0, stream, a);
+    ATTS_LAUNCH_CHECK("quant_kernel");
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(quant_join_kernel<T>, dim3((unsigned)ceil_div((int64_t)a.M * a.N, 256)), dim3(256), 0, stream, a);
+        ATTS_LAUNCH_CHECK("quant_join_kernel");
+    }
     return ATTS_OK;
 }
 
 template <typename T>
-int32_t launch_quant_epi(int32_t epilogue, const QuantArgs& a, hipStream_t stream) {
-    switch (epilogue) {
-        case ATTS_EPILOGUE_STORE: return launch_quant<T, ATTS_EPILOGUE_STORE>(a, stream);
-        case ATTS_EPILOGUE_STORE_F32: return launch_quant<T, ATTS_EPILOGUE_STORE_F32>(a, stream);
-        case ATTS_EPILOGUE_RESIDUAL: return launch_quant<T, ATTS_EPILOGUE_RESIDUAL>(a, stream);
-        default: return launch_quant<T, ATTS_EPILOGUE_SWIGLU>(a, stream);
-    }
+int32_t launch_quant_group(int32_t group, const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
+    return group == 32 ? launch_quant<T, 32>(p, a, stream) : group == 64 ? launch_quant<T, 64>(p, a, stream) : launch_quant<T, 128>(p, a, stream);
 }
 
 // Eight lanes a group: each holds group / 8 of its values, their limits are joined by three exchanges.
@@ -121,7 +343,7 @@ int32_t check_quant(const char* fn, int32_t dtype, int32_t N, int32_t Kdim, int3
     if (N < 1 || Kdim < 1) return fail(ATTS_ERR_INVALID_ARG, "%s: need N and Kdim >= 1", fn);
     if ((group != 32 && group != 64 && group != 128) || Kdim % group)
         return fail(ATTS_ERR_SHAPE, "%s: group = %d is not 32, 64 or 128, or does not divide Kdim = %d", fn, group, Kdim);
-    if (N > (1 << 29) || Kdim > (1 << 29)) return fail(ATTS_ERR_SHAPE, "%s: N or Kdim exceeds 2^29", fn);
+    if (N > (1 << 29) || Kdim > (1 << 24)) return fail(ATTS_ERR_SHAPE, "%s: N exceeds 2^29 or Kdim 2^24", fn);
     return ATTS_OK;
 }
 
@@ -132,9 +354,19 @@ using namespace atts;
 
 extern "C" {
 
+int32_t atts_gemm_nt_quant_workspace_bytes(int32_t dtype, int32_t M, int32_t N, int32_t Kdim, int32_t epilogue, size_t* out_bytes) {
+    const char* fn = "atts_gemm_nt_quant_workspace_bytes";
+    if (!out_bytes) return fail(ATTS_ERR_INVALID_ARG, "%s: out_bytes is NULL", fn);
+    if (dtype != ATTS_DTYPE_F32 && dtype != ATTS_DTYPE_BF16) return fail(ATTS_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, dtype);
+    if (M < 0 || N < 1 || Kdim < 1 || N > (1 << 29) || Kdim > (1 << 24)) return fail(ATTS_ERR_INVALID_ARG, "%s: need M >= 0, N in [1, 2^29], Kdim in [1, 2^24]", fn);
+    if (epilogue < ATTS_EPILOGUE_STORE || epilogue > ATTS_EPILOGUE_SWIGLU) return fail(ATTS_ERR_INVALID_ARG, "%s: unknown epilogue %d", fn, epilogue);
+    *out_bytes = M == 0 ? 0 : align_up(quant_plan(dtype, M, N, Kdim, epilogue).bytes, 256);
+    return ATTS_OK;
+}
+
 int32_t atts_gemm_nt_quant(int32_t dtype, const void* x, int64_t x_stride, const uint8_t* codes, const void* scales, const uint8_t* zeros,
                            int32_t group, const float* residual, void* out, int32_t M, int32_t N, int32_t Kdim, int32_t epilogue,
-                           void* hip_stream) {
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
     const char* fn = "atts_gemm_nt_quant";
     const int32_t rc = check_quant(fn, dtype, N, Kdim, group);
     if (rc != ATTS_OK) return rc;
@@ -143,11 +375,16 @@ int32_t atts_gemm_nt_quant(int32_t dtype, const void* x, int64_t x_stride, const
     if (M == 0) return ATTS_OK;
     if (!x || !codes || !scales || !out || (epilogue == ATTS_EPILOGUE_RESIDUAL && !residual)) return fail(ATTS_ERR_INVALID_ARG, "%s: NULL argument", fn);
     if (x_stride < Kdim) return fail(ATTS_ERR_INVALID_ARG, "%s: rows of x overlap", fn);
+    if (x_stride > (1 << 25)) return fail(ATTS_ERR_SHAPE, "%s: x_stride = %lld exceeds 2^25", fn, (long long)x_stride);
     if (((uintptr_t)x | (uintptr_t)codes | ((uint64_t)x_stride * dtype_size(dtype))) & 15)
         return fail(ATTS_ERR_INVALID_ARG, "%s: x, its rows and codes must be 16-byte aligned", fn);
-    const QuantArgs a{x, codes, scales, zeros, residual, out, x_stride, M, N, Kdim, group == 32 ? 5 : group == 64 ? 6 : 7, Kdim / group};
+    const QuantPlan p = quant_plan(dtype, M, N, Kdim, epilogue);
+    if (p.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.bytes))
+        return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, p.bytes);
+    const QuantArgs a{x, codes, scales, zeros, residual, out, static_cast<float*>(workspace), x_stride, M, N, Kdim, Kdim / group, epilogue,
+                      epilogue == ATTS_EPILOGUE_SWIGLU ? 2 * N : N, p.splits, p.steps_per_split, p.steps, p.row_blocks, p.tiles};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return dtype == ATTS_DTYPE_F32 ? launch_quant_epi<float>(epilogue, a, stream) : launch_quant_epi<bf16>(epilogue, a, stream);
+    return dtype == ATTS_DTYPE_F32 ? launch_quant_group<float>(group, p, a, stream) : launch_quant_group<bf16>(group, p, a, stream);
 }
 
 int32_t atts_quantize_rows(int32_t dtype, const void* w, int32_t N, int32_t Kdim, int32_t group, uint8_t* codes, void* scales, uint8_t* zeros,

@@ -42,7 +42,7 @@ def test_null_and_misaligned_arguments():
     assert LIB.atts_rotary_append(_desc(), ONE, 100, ONE, ONE, ONE, 5, 8, ONE, 1, 16, 0, ONE, None) == A.ERR_INVALID_ARG          # rows overlap
     assert LIB.atts_rotary_append(_desc(), ONE, 1 << 20, ONE, ONE, ONE, 5, 8, None, 1, 16, 0, ONE, None) == A.ERR_INVALID_ARG
     assert LIB.atts_rotary_append(_desc(), ONE, 1 << 20, ONE, ONE, ONE, 5, 8, ONE, 1, 130, 0, ONE, None) == A.ERR_SHAPE
-    quant = lambda *a: LIB.atts_gemm_nt_quant(*a)
+    quant = lambda *a: LIB.atts_gemm_nt_quant(*a[:-1], ONE, 1 << 40, None)
     assert quant(1, ONE, 256, ONE, ONE, None, 64, None, ONE, 0, 8, 256, 0, None) == 0                                             # no rows
     assert quant(2, ONE, 256, ONE, ONE, None, 64, None, ONE, 4, 8, 256, 0, None) == A.ERR_INVALID_ARG
     assert quant(1, ONE, 256, ONE, ONE, None, 48, None, ONE, 4, 8, 96, 0, None) == A.ERR_SHAPE
