@@ -1,6 +1,8 @@
 // Products of a few rows with weights in 4 bits:  out = X W^T,  W[n, k] = scale[n, k / G] (code[n, k] - zero[n, k / G]).
 #include "common.h"
 
+#include <type_traits>
+
 namespace atts {
 namespace {
 
@@ -17,7 +19,7 @@ struct QuantArgs {
     int32_t splits, steps_per_split, steps, row_blocks, tiles;
 };
 
-constexpr int kQuantWaves = 8;
+constexpr int kStageBytes = 65536;
 constexpr int kSpan = 128;       // K elements of a step: 16 bytes of codes a lane
 
 __device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
@@ -44,11 +46,19 @@ __device__ __forceinline__ bf16x8 in_code_order(const uint4& d) {
 template <typename T> struct Parts;
 template <> struct Parts<bf16> {
     static constexpr int kN = 1, kLoads = 1;
+    typedef uint32_t Scale;                                                 // the scale's 16 bits, then 16 + zero
+    static __device__ Scale pack(bf16 scale, uint32_t zero) { return (uint32_t)__builtin_bit_cast(uint16_t, scale) << 16 | (16 + zero); }
+    static __device__ float scale_of(Scale s) { return __uint_as_float(s & 0xffff0000u); }
+    static __device__ float zero_of(Scale s) { return (float)(s & 0xffffu); }
     bf16x8 v[1];
     __device__ explicit Parts(const uint4* raw) { v[0] = in_code_order(raw[0]); }
 };
 template <> struct Parts<float> {
     static constexpr int kN = 3, kLoads = 2;
+    typedef float2 Scale;
+    static __device__ Scale pack(float scale, uint32_t zero) { return make_float2(scale, (float)(16 + zero)); }
+    static __device__ float scale_of(Scale s) { return s.x; }
+    static __device__ float zero_of(Scale s) { return s.y; }
     bf16x8 v[3];
     __device__ explicit Parts(const uint4* raw) {
         const f32x4 lo = __builtin_bit_cast(f32x4, raw[0]), hi = __builtin_bit_cast(f32x4, raw[1]);
@@ -65,12 +75,13 @@ template <> struct Parts<float> {
 };
 
 // Eight codes as 16 + code, exact in 16 bits: the code goes to the upper four of the seven stored bits of 16 = 0x4180.
-__device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
+// The constants come in registers: as literals they would make two instructions of every mask.
+__device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w, uint32_t mask, uint32_t sixteen) {
     uint4 o;
-    o.x = (w << 3 & 0x00780078u) | 0x41804180u;
-    o.y = (w >> 1 & 0x00780078u) | 0x41804180u;
-    o.z = (w >> 5 & 0x00780078u) | 0x41804180u;
-    o.w = (w >> 9 & 0x00780078u) | 0x41804180u;
+    o.x = (w << 3 & mask) | sixteen;
+    o.y = (w >> 1 & mask) | sixteen;
+    o.z = (w >> 5 & mask) | sixteen;
+    o.w = (w >> 9 & mask) | sixteen;
     return __builtin_bit_cast(bf16x8, o);
 }
 
@@ -84,30 +95,41 @@ __device__ __forceinline__ void swap_quarters(uint4& w) {
 }
 
 // A workgroup: NS blocks of 16 weight rows (SwiGLU: gate and up blocks in turn) times MT blocks of 16 rows of X, over one split of K; its wavefronts
-// take every eighth step.  G: group size.
-template <typename T, int G, int NS, int MT>
-__global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a) {
+// take every W-th step.  G: group size.
+template <typename T, int G, int NS, int MT, int W>
+__global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
     using P = Parts<T>;
     constexpr int kGroups = kSpan / G, kRows = 16 * MT, kCols = 16 * NS, kPitch = kCols + 4;
-    __shared__ float red[kQuantWaves][16][kPitch];
+    // Scales and zeros of as many steps as fit, [group][weight row]: a lane's own, two bytes of a row each, would cost as many cache lines a step as
+    // the codes do.  Behind the loop the sums of the wavefronts.
+    constexpr int kStage = kStageBytes / sizeof(typename P::Scale), kScalePitch = kCols + 1;
+    constexpr int kStageSteps = kStage / (kScalePitch * kGroups) / (2 * W) * (2 * W);     // whole pairs of steps
+    static_assert(kStageSteps > 0);
+    __shared__ union {
+        typename P::Scale scale[kStage];
+        float red[W][16][kPitch];
+    } lds;
     // Workgroups of the same weights and other rows of X lie 8 apart: the same XCD, and so the same L2.
     const int id = blockIdx.x, row_block = id / 8 % a.row_blocks, cell = id / (8 * a.row_blocks) * 8 + id % 8;
     if (cell >= a.tiles * a.splits) return;
     const int tile = cell % a.tiles, split = cell / a.tiles;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, c = lane >> 4;
     const bool swiglu = a.epilogue == ATTS_EPILOGUE_SWIGLU;
-    const int m0 = row_block * kRows, t0 = split * a.steps_per_split + wave, t1 = min((split + 1) * a.steps_per_split, a.steps);
+    const int m0 = row_block * kRows, t0 = split * a.steps_per_split, t1 = min((split + 1) * a.steps_per_split, a.steps);
 
     // Every address is a base that the whole workgroup shares and an offset of 32 bits.  Block s begins at weight row first[s]; rows past the
     // last one are read as it, here and in X, and dropped at the end.
+    const auto first_row = [&](int s) {
+        const int n = swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16;
+        return min(n, a.N - 1) + (swiglu ? (int64_t)(s & 1) * a.N : 0);     // the block itself may lie behind the end
+    };
+    const auto last_row = [&](int s) { return max(0, a.N - 1 - (swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16)); };
     int64_t first[NS];
     uint32_t row[NS], x_at[MT];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const int n = swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16;
-        const int in = max(0, min(n, a.N - 1));                             // the block itself may lie behind the end
-        first[s] = in + (swiglu ? (int64_t)(s & 1) * a.N : 0);
-        row[s] = (uint32_t)min(r, a.N - 1 - in);
+        first[s] = first_row(s);
+        row[s] = (uint32_t)min(r, last_row(s));
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) x_at[m] = (uint32_t)(min(m * 16 + r, a.M - 1 - m0) * a.x_stride + c * 8) * sizeof(T);
@@ -115,8 +137,6 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
 
     struct Step {
         uint4 w[NS], x[MT][4][P::kLoads];
-        struct { T v[kGroups]; } scale[NS];
-        struct { uint8_t v[kGroups]; } zero[NS];
     };
     auto load = [&](Step& f, int t) __attribute__((always_inline)) {
         const int k = min(t, t1 - 1) * kSpan;                               // past the end: a repeat, not used
@@ -124,24 +144,6 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
 #pragma unroll
         for (int s = 0; s < NS; ++s)
             f.w[s] = *reinterpret_cast<const uint4*>(a.codes + first[s] * (a.K / 2) + k / 2 + (row[s] * (uint32_t)(a.K / 2) + mine));
-        const T* scales = reinterpret_cast<const T*>(a.scales) + k / G;
-        if (k + kSpan <= a.K) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const uint32_t at = row[s] * (uint32_t)a.groups;
-                __builtin_memcpy(&f.scale[s], scales + first[s] * a.groups + at, sizeof(f.scale[s]));
-                if (a.zeros) __builtin_memcpy(&f.zero[s], a.zeros + first[s] * a.groups + k / G + at, sizeof(f.zero[s]));
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < NS; ++s)
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g) {
-                    const uint32_t at = row[s] * (uint32_t)a.groups + min(g, a.groups - 1 - k / G);
-                    f.scale[s].v[g] = scales[first[s] * a.groups + at];
-                    if (a.zeros) f.zero[s].v[g] = a.zeros[first[s] * a.groups + k / G + at];
-                }
-        }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -156,14 +158,18 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[s][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
-    auto use = [&](Step& f, int t) __attribute__((always_inline)) {
-        if (t >= t1) return;                                                // wave-uniform
+    uint32_t mask, sixteen;
+    asm("s_mov_b32 %0, 0x00780078" : "=s"(mask));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
+    int staged = 0;                                                         // first step whose scales are in LDS
+    auto products = [&](Step& f, int t, auto whole) __attribute__((always_inline)) {
+        const typename P::Scale* mine = lds.scale + (t - staged) * kGroups * kScalePitch + r;
         f32x4 sum[NS][MT], sx[MT];
 #pragma unroll
         for (int s = 0; s < NS; ++s) swap_quarters(f.w[s]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j > 0 && t * kSpan + j * 32 >= a.K) break;                  // wave-uniform
+            if (!decltype(whole)::value && t * kSpan + j * 32 >= a.K) break;    // wave-uniform
             if (j * 32 % G == 0) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
             }
             bf16x8 w[NS];
 #pragma unroll
-            for (int s = 0; s < NS; ++s) w[s] = codes_plus_16(j == 0 ? f.w[s].x : j == 1 ? f.w[s].y : j == 2 ? f.w[s].z : f.w[s].w);
+            for (int s = 0; s < NS; ++s) w[s] = codes_plus_16(j == 0 ? f.w[s].x : j == 1 ? f.w[s].y : j == 2 ? f.w[s].z : f.w[s].w, mask, sixteen);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const P part(f.x[m][j]);
@@ -188,7 +194,8 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
             if ((j + 1) * 32 % G == 0) {
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
-                    const float scale = to_f32(f.scale[s].v[j * 32 / G]), zero = a.zeros ? 16.f + (float)f.zero[s].v[j * 32 / G] : 24.f;
+                    const typename P::Scale own = mine[j * 32 / G * kScalePitch + s * 16];
+                    const float scale = P::scale_of(own), zero = P::zero_of(own);
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -198,17 +205,49 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
         }
     };
 
+    const auto stage = [&](int from, int steps) {
+        const int n = min(steps * kGroups, a.groups - from * kGroups);
+        const uint8_t* const zeros = a.zeros ? a.zeros : a.codes;           // loaded on either path, so that the loads need no branch
+        constexpr int kEach = (kCols + W - 1) / W;       // weight rows of a wavefront, its lanes side by side along the groups
+        for (int g0 = 0; g0 < n; g0 += 64) {
+            const int g = min(g0 + lane, n - 1);
+            T scale[kEach];
+            uint8_t zero[kEach];
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const int i = wave + u * W, s = i >> 4;           // rows past the last one repeat it
+                const int64_t at = (first_row(s) + min(i & 15, last_row(s))) * a.groups + from * kGroups + g;
+                scale[u] = reinterpret_cast<const T*>(a.scales)[at];
+                zero[u] = zeros[at];
+            }
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+                if (g0 + lane < n) lds.scale[g * kScalePitch + wave + u * W] = P::pack(scale[u], a.zeros ? zero[u] : 8);
+        }
+    };
+
+    // Two steps are under way in two sets of registers.  The loop has no branch inside, or the waits would be for everything; what does not make
+    // a pair of whole steps is left for the end.
     Step fa, fb;
-    if (t0 < t1) {
-        load(fa, t0);
-        load(fb, t0 + kQuantWaves);
-        for (int t = t0; t < t1; t += 2 * kQuantWaves) {
-            use(fa, t);
-            load(fa, t + 2 * kQuantWaves);
-            use(fb, t + kQuantWaves);
-            load(fb, t + 3 * kQuantWaves);
+    int t = t0 + wave;
+    load(fa, t);
+    load(fb, t + W);
+    for (int from = t0; from < t1; from += kStageSteps) {
+        const int end = min(from + kStageSteps, t1), whole = min(end, a.K / kSpan);
+        if (from > t0) __syncthreads();
+        stage(from, end - from);
+        staged = from;
+        __syncthreads();
+        for (; t + W < whole; t += 2 * W) {
+            products(fa, t, std::true_type{});
+            load(fa, t + 2 * W);
+            products(fb, t + W, std::true_type{});
+            load(fb, t + 3 * W);
         }
     }
+    if (t < t1) products(fa, t, std::false_type{});
+    if (t + W < t1) products(fb, t + W, std::false_type{});
+    __syncthreads();
 
     // acc[s][m][i]: row 4 c + i of block m, column r of block s.  The wavefronts' sums are added in their order.
 #pragma unroll
@@ -217,16 +256,16 @@ __global__ __launch_bounds__(64 * kQuantWaves, 2) void quant_kernel(QuantArgs a)
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) red[wave][4 * c + i][s * 16 + r] = acc[s][m][i];
+            for (int i = 0; i < 4; ++i) lds.red[wave][4 * c + i][s * 16 + r] = acc[s][m][i];
         __syncthreads();
         const int outs = swiglu && a.splits == 1 ? kCols / 2 : kCols;
-        for (int e = tid; e < 16 * outs; e += 64 * kQuantWaves) {
+        for (int e = tid; e < 16 * outs; e += 64 * W) {
             const int row = e / outs, o = e - row * outs, mrow = m0 + m * 16 + row;
             if (mrow >= a.M) continue;
             auto total = [&](int col) {
                 float y = 0.f;
 #pragma unroll
-                for (int w = 0; w < kQuantWaves; ++w) y += red[w][row][col];
+                for (int w = 0; w < W; ++w) y += lds.red[w][row][col];
                 return y;
             };
             if (a.splits > 1) {
@@ -258,7 +297,7 @@ __global__ __launch_bounds__(256) void quant_join_kernel(QuantArgs a) {
 
 // How a call is cut.
 struct QuantPlan {
-    int32_t ns, mt, tiles, splits, steps, steps_per_split, row_blocks;
+    int32_t ns, mt, waves, tiles, splits, steps, steps_per_split, row_blocks;
     size_t bytes;
 };
 
@@ -269,13 +308,14 @@ QuantPlan quant_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t epi
     p.mt = M <= 16 || dtype == ATTS_DTYPE_F32 ? 1 : 2;     // fp32: three parts of X and their sums leave no room for a second block
     p.row_blocks = (int32_t)ceil_div(M, 16 * p.mt);
     p.ns = M > 16 || ceil_div(wide, 64) >= kChip ? 4 : epilogue == ATTS_EPILOGUE_SWIGLU || ceil_div(wide, 32) >= kChip ? 2 : 1;
+    p.waves = p.ns == 4 ? 4 : 8;
     const int64_t tiles = ceil_div(wide, 16 * p.ns);
     p.tiles = (int32_t)(epilogue == ATTS_EPILOGUE_SWIGLU ? ceil_div(N, 8 * p.ns) : tiles);
     p.steps = (int32_t)ceil_div(K, kSpan);
     int64_t splits = 1;
     if (M > 16) {
-        splits = kChip / ((int64_t)p.tiles * p.row_blocks);
-        const int64_t most = p.steps / (2 * kQuantWaves);     // two steps a wavefront at least
+        splits = 2 * kChip / ((int64_t)p.tiles * p.row_blocks);
+        const int64_t most = p.steps / (2 * p.waves);     // two steps a wavefront at least
         if (splits > most) splits = most;
         if (splits < 1) splits = 1;
     }
@@ -289,11 +329,10 @@ template <typename T, int G>
 int32_t launch_quant(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
     const int64_t wgs = ceil_div((int64_t)p.tiles * p.splits, 8) * 8 * p.row_blocks;
     if (wgs > 0x7fffffff) return fail(ATTS_ERR_SHAPE, "atts_gemm_nt_quant: the call has more than 2^31 workgroups");
-    const dim3 grid((unsigned)wgs), block(64 * kQuantWaves);
-    if (p.mt == 2) hipLaunchKernelGGL((quant_kernel<T, G, 4, sizeof(T) == 2 ? 2 : 1>), grid, block, 0, stream, a);
-    else if (p.ns == 4) hipLaunchKernelGGL((quant_kernel<T, G, 4, 1>), grid, block, 0, stream, a);
-    else if (p.ns == 2) hipLaunchKernelGGL((quant_kernel<T, G, 2, 1>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((quant_kernel<T, G, 1, 1>), grid, block, 0, stream, a);
+    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * p.waves), 0, stream, a); };
+    if (p.mt == 2) run(quant_kernel<T, G, 4, sizeof(T) == 2 ? 2 : 1, 4>);
+    else if (p.ns == 4) run(quant_kernel<T, G, 4, 1, 4>);
+    else run(p.ns == 2 ? quant_kernel<T, G, 2, 1, 8> : quant_kernel<T, G, 1, 1, 8>);
     ATTS_LAUNCH_CHECK("quant_kernel");
     if (p.splits > 1) {
         hipLaunchKernelGGL(quant_join_kernel<T>, dim3((unsigned)ceil_div((int64_t)a.M * a.N, 256)), dim3(256), 0, stream, a);
