@@ -19,7 +19,9 @@ struct QuantArgs {
     int32_t splits, steps_per_split, steps, row_blocks, tiles;
 };
 
-constexpr int kStageBytes = 65536;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kStageBytes = 32768;
 constexpr int kSpan = 128;       // K elements of a step: 16 bytes of codes a lane
 
 __device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
@@ -33,12 +35,9 @@ __device__ __forceinline__ void finish(const QuantArgs& a, int m, int n, float y
 }
 
 // Eight activations as they meet the codes of a word: 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ bf16x8 in_code_order(const uint4& d) {
-    uint4 o;
-    o.x = __builtin_amdgcn_perm(d.z, d.x, 0x05040100u);
-    o.y = __builtin_amdgcn_perm(d.z, d.x, 0x07060302u);
-    o.z = __builtin_amdgcn_perm(d.w, d.y, 0x05040100u);
-    o.w = __builtin_amdgcn_perm(d.w, d.y, 0x07060302u);
+__device__ __forceinline__ bf16x8 in_code_order(const u32x4& d) {
+    const u32x4 o = {__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
+                     __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)};
     return __builtin_bit_cast(bf16x8, o);
 }
 
@@ -51,7 +50,7 @@ template <> struct Parts<bf16> {
     static __device__ float scale_of(Scale s) { return __uint_as_float(s & 0xffff0000u); }
     static __device__ float zero_of(Scale s) { return (float)(s & 0xffffu); }
     bf16x8 v[1];
-    __device__ explicit Parts(const uint4* raw) { v[0] = in_code_order(raw[0]); }
+    __device__ explicit Parts(const u32x4* raw) { v[0] = in_code_order(raw[0]); }
 };
 template <> struct Parts<float> {
     static constexpr int kN = 3, kLoads = 2;
@@ -60,7 +59,7 @@ template <> struct Parts<float> {
     static __device__ float scale_of(Scale s) { return s.x; }
     static __device__ float zero_of(Scale s) { return s.y; }
     bf16x8 v[3];
-    __device__ explicit Parts(const uint4* raw) {
+    __device__ explicit Parts(const u32x4* raw) {
         const f32x4 lo = __builtin_bit_cast(f32x4, raw[0]), hi = __builtin_bit_cast(f32x4, raw[1]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -86,12 +85,12 @@ __device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w, uint32_t mask, uint3
 }
 
 // Word j of quarter-wave c for word c of quarter-wave j.
-__device__ __forceinline__ void swap_quarters(uint4& w) {
-    const auto a = __builtin_amdgcn_permlane32_swap(w.x, w.z, false, false);
-    const auto b = __builtin_amdgcn_permlane32_swap(w.y, w.w, false, false);
+__device__ __forceinline__ void swap_quarters(u32x4& w) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
     const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    w = make_uint4(c[0], c[1], d[0], d[1]);
+    w = u32x4{c[0], c[1], d[0], d[1]};
 }
 
 // A workgroup: NS blocks of 16 weight rows (SwiGLU: gate and up blocks in turn) times MT blocks of 16 rows of X, over one split of K; its wavefronts
@@ -109,6 +108,7 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
         typename P::Scale scale[kStage];
         float red[W][16][kPitch];
     } lds;
+    __shared__ u32x4 turn[W][NS * 64 + MT * P::kLoads * 256];               // a step of codes and activations on its way from rows to fragments
     // Workgroups of the same weights and other rows of X lie 8 apart: the same XCD, and so the same L2.
     const int id = blockIdx.x, row_block = id / 8 % a.row_blocks, cell = id / (8 * a.row_blocks) * 8 + id % 8;
     if (cell >= a.tiles * a.splits) return;
@@ -124,33 +124,35 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
         return min(n, a.N - 1) + (swiglu ? (int64_t)(s & 1) * a.N : 0);     // the block itself may lie behind the end
     };
     const auto last_row = [&](int s) { return max(0, a.N - 1 - (swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16)); };
+    // Memory is read by rows: four lanes a weight row (64 bytes), kXLanes a row of X, so that neighbours share a cache line.
+    constexpr int kXLanes = kSpan * sizeof(T) / 16, kXLoads = 16 * kXLanes / 64;
     int64_t first[NS];
-    uint32_t row[NS], x_at[MT];
+    uint32_t at_w[NS], at_x[MT][kXLoads];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         first[s] = first_row(s);
-        row[s] = (uint32_t)min(r, last_row(s));
+        at_w[s] = (uint32_t)min(lane >> 2, last_row(s)) * (uint32_t)(a.K / 2);
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m) x_at[m] = (uint32_t)(min(m * 16 + r, a.M - 1 - m0) * a.x_stride + c * 8) * sizeof(T);
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i)
+            at_x[m][i] = (uint32_t)min(m * 16 + (i * 64 + lane) / kXLanes, a.M - 1 - m0) * (uint32_t)(a.x_stride * sizeof(T));
     const char* const x0 = reinterpret_cast<const char*>(a.x) + m0 * a.x_stride * (int64_t)sizeof(T);
 
     struct Step {
-        uint4 w[NS], x[MT][4][P::kLoads];
+        u32x4 w[NS], x[MT][kXLoads];
     };
     auto load = [&](Step& f, int t) __attribute__((always_inline)) {
         const int k = min(t, t1 - 1) * kSpan;                               // past the end: a repeat, not used
-        const uint32_t mine = k + c * 32 < a.K ? c * 16 : 0;                // a last step may be partly filled
+        const uint32_t own_w = k + (lane & 3) * 32 < a.K ? (lane & 3) * 16 : 0;     // a last step may be partly filled
+        const uint32_t own_x = k + lane % kXLanes * (16 / (int)sizeof(T)) < a.K ? lane % kXLanes * 16 : 0;
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-            f.w[s] = *reinterpret_cast<const uint4*>(a.codes + first[s] * (a.K / 2) + k / 2 + (row[s] * (uint32_t)(a.K / 2) + mine));
+        for (int s = 0; s < NS; ++s) f.w[s] = *reinterpret_cast<const u32x4*>(a.codes + first[s] * (a.K / 2) + k / 2 + (at_w[s] + own_w));
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < P::kLoads; ++i)
-                    f.x[m][j][i] = *reinterpret_cast<const uint4*>(x0 + (int64_t)(k + (k + j * 32 < a.K ? j * 32 : 0)) * sizeof(T) + i * 16 + x_at[m]);
+            for (int i = 0; i < kXLoads; ++i) f.x[m][i] = *reinterpret_cast<const u32x4*>(x0 + (int64_t)k * sizeof(T) + (at_x[m][i] + own_x));
     };
     f32x4 acc[NS][MT];
 #pragma unroll
@@ -164,9 +166,26 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
     int staged = 0;                                                         // first step whose scales are in LDS
     auto products = [&](Step& f, int t, auto whole) __attribute__((always_inline)) {
         const typename P::Scale* mine = lds.scale + (t - staged) * kGroups * kScalePitch + r;
-        f32x4 sum[NS][MT], sx[MT];
+        // Rows to fragments through LDS; a wavefront's accesses to it are done in their order, so nothing has to be waited for between them.  A
+        // piece of 16 bytes lies where eight rows' pieces that are read together fall into different banks.
+        u32x4* const own = turn[wave];
+        u32x4* const own_x = own + NS * 64;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) swap_quarters(f.w[s]);
+        for (int s = 0; s < NS; ++s) own[s * 64 + (lane & ~3) + ((lane & 3) ^ (lane >> 3 & 3))] = f.w[s];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < kXLoads; ++i) {
+                const int row = (i * 64 + lane) / kXLanes;
+                own_x[(m * 16 + row) * kXLanes + (lane % kXLanes ^ (row & 7))] = f.x[m][i];
+            }
+        u32x4 code[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            code[s] = own[s * 64 + r * 4 + (c ^ (r >> 1 & 3))];
+            if (G < kSpan) swap_quarters(code[s]);
+        }
+        f32x4 sum[NS][MT], sx[MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (!decltype(whole)::value && t * kSpan + j * 32 >= a.K) break;    // wave-uniform
@@ -180,10 +199,16 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
             }
             bf16x8 w[NS];
 #pragma unroll
-            for (int s = 0; s < NS; ++s) w[s] = codes_plus_16(j == 0 ? f.w[s].x : j == 1 ? f.w[s].y : j == 2 ? f.w[s].z : f.w[s].w, mask, sixteen);
+            for (int s = 0; s < NS; ++s) w[s] = codes_plus_16(code[s][j], mask, sixteen);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const P part(f.x[m][j]);
+                u32x4 raw[P::kLoads];
+#pragma unroll
+                for (int i = 0; i < P::kLoads; ++i) {
+                    const int piece = (G < kSpan ? 4 * j + c : 4 * c + j) * P::kLoads + i;
+                    raw[i] = own_x[(m * 16 + r) * kXLanes + (piece ^ (r & 7))];
+                }
+                const P part(raw);
 #pragma unroll
                 for (int i = 0; i < P::kN; ++i) {
                     sx[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part.v[i], ones, sx[m], 0, 0, 0);
