@@ -16,7 +16,7 @@ struct QuantArgs {
     float* parts;                // K cut over workgroups: their sums, [splits][M][rows of W]
     int64_t x_stride;
     int32_t M, N, K, groups, epilogue, wide;      // wide: rows of W
-    int32_t splits, steps_per_split, steps, row_blocks, tiles;
+    int32_t splits, steps_per_split, steps, row_blocks, tiles, stage_steps;
 };
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -93,22 +93,38 @@ __device__ __forceinline__ void swap_quarters(u32x4& w) {
     w = u32x4{c[0], c[1], d[0], d[1]};
 }
 
+// Wavefronts a SIMD is to hold: what the registers of a shape allow without spilling.
+template <typename T, int NS, int MT>
+struct QuantWaves {
+    static constexpr int kN = NS == 4 ? (MT == 1 && sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? (NS == 1 ? 5 : 4) : 3;
+};
+
+// A workgroup's LDS: the turn of each wavefront, then scales, and behind the loop sums in their place.
+template <typename T, int G, int NS, int MT, int W>
+struct QuantLds {
+    static constexpr int kGroups = kSpan / G, kScalePitch = 16 * NS + 1;
+    static constexpr int kTurn = W * (NS * 64 + MT * Parts<T>::kLoads * 256) * 16, kRed = W * 16 * (16 * NS + 4) * 4;
+    static constexpr int kStep = kGroups * kScalePitch * (int)sizeof(typename Parts<T>::Scale);      // scales of a step
+    static constexpr int kMost = kStageBytes / kStep / (2 * W) * (2 * W);                            // whole pairs of steps of every wavefront
+    static_assert(kMost > 0);
+    static int steps(int n) { return n < kMost ? (n + 2 * W - 1) / (2 * W) * (2 * W) : kMost; }
+    static size_t bytes(int n) { return kTurn + (n * kStep > kRed ? n * kStep : kRed); }
+};
+
 // A workgroup: NS blocks of 16 weight rows (SwiGLU: gate and up blocks in turn) times MT blocks of 16 rows of X, over one split of K; its wavefronts
 // take every W-th step.  G: group size.
 template <typename T, int G, int NS, int MT, int W>
-__global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
+__global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_kernel(QuantArgs a) {
     using P = Parts<T>;
     constexpr int kGroups = kSpan / G, kRows = 16 * MT, kCols = 16 * NS, kPitch = kCols + 4;
     // Scales and zeros of as many steps as fit, [group][weight row]: a lane's own, two bytes of a row each, would cost as many cache lines a step as
     // the codes do.  Behind the loop the sums of the wavefronts.
-    constexpr int kStage = kStageBytes / sizeof(typename P::Scale), kScalePitch = kCols + 1;
-    constexpr int kStageSteps = kStage / (kScalePitch * kGroups) / (2 * W) * (2 * W);     // whole pairs of steps
-    static_assert(kStageSteps > 0);
-    __shared__ union {
-        typename P::Scale scale[kStage];
-        float red[W][16][kPitch];
-    } lds;
-    __shared__ u32x4 turn[W][NS * 64 + MT * P::kLoads * 256];               // a step of codes and activations on its way from rows to fragments
+    using L = QuantLds<T, G, NS, MT, W>;
+    constexpr int kScalePitch = L::kScalePitch;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    u32x4* const turn = reinterpret_cast<u32x4*>(smem);                     // a step of codes and activations on its way from rows to fragments
+    typename P::Scale* const lds_scale = reinterpret_cast<typename P::Scale*>(smem + L::kTurn);
+    float (*const red)[16][kPitch] = reinterpret_cast<float (*)[16][kPitch]>(smem + L::kTurn);
     // Workgroups of the same weights and other rows of X lie 8 apart: the same XCD, and so the same L2.
     const int id = blockIdx.x, row_block = id / 8 % a.row_blocks, cell = id / (8 * a.row_blocks) * 8 + id % 8;
     if (cell >= a.tiles * a.splits) return;
@@ -165,10 +181,10 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
     asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
     int staged = 0;                                                         // first step whose scales are in LDS
     auto products = [&](Step& f, int t, auto whole) __attribute__((always_inline)) {
-        const typename P::Scale* mine = lds.scale + (t - staged) * kGroups * kScalePitch + r;
+        const typename P::Scale* mine = lds_scale + (t - staged) * kGroups * kScalePitch + r;
         // Rows to fragments through LDS; a wavefront's accesses to it are done in their order, so nothing has to be waited for between them.  A
         // piece of 16 bytes lies where eight rows' pieces that are read together fall into different banks.
-        u32x4* const own = turn[wave];
+        u32x4* const own = turn + wave * (NS * 64 + MT * P::kLoads * 256);
         u32x4* const own_x = own + NS * 64;
 #pragma unroll
         for (int s = 0; s < NS; ++s) own[s * 64 + (lane & ~3) + ((lane & 3) ^ (lane >> 3 & 3))] = f.w[s];
@@ -247,7 +263,7 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < kEach; ++u)
-                if (g0 + lane < n) lds.scale[g * kScalePitch + wave + u * W] = P::pack(scale[u], a.zeros ? zero[u] : 8);
+                if (g0 + lane < n) lds_scale[g * kScalePitch + wave + u * W] = P::pack(scale[u], a.zeros ? zero[u] : 8);
         }
     };
 
@@ -257,8 +273,8 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
     int t = t0 + wave;
     load(fa, t);
     load(fb, t + W);
-    for (int from = t0; from < t1; from += kStageSteps) {
-        const int end = min(from + kStageSteps, t1), whole = min(end, a.K / kSpan);
+    for (int from = t0; from < t1; from += a.stage_steps) {
+        const int end = min(from + a.stage_steps, t1), whole = min(end, a.K / kSpan);
         if (from > t0) __syncthreads();
         stage(from, end - from);
         staged = from;
@@ -281,7 +297,7 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) lds.red[wave][4 * c + i][s * 16 + r] = acc[s][m][i];
+            for (int i = 0; i < 4; ++i) red[wave][4 * c + i][s * 16 + r] = acc[s][m][i];
         __syncthreads();
         const int outs = swiglu && a.splits == 1 ? kCols / 2 : kCols;
         for (int e = tid; e < 16 * outs; e += 64 * W) {
@@ -290,7 +306,7 @@ __global__ __launch_bounds__(64 * W, 2) void quant_kernel(QuantArgs a) {
             auto total = [&](int col) {
                 float y = 0.f;
 #pragma unroll
-                for (int w = 0; w < W; ++w) y += lds.red[w][row][col];
+                for (int w = 0; w < W; ++w) y += red[w][row][col];
                 return y;
             };
             if (a.splits > 1) {
@@ -350,14 +366,15 @@ QuantPlan quant_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t epi
     return p;
 }
 
-template <typename T, int G>
-int32_t launch_quant(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
+template <typename T, int G, int NS, int MT, int W>
+int32_t launch_quant(const QuantPlan& p, QuantArgs a, hipStream_t stream) {
+    using L = QuantLds<T, G, NS, MT, W>;
     const int64_t wgs = ceil_div((int64_t)p.tiles * p.splits, 8) * 8 * p.row_blocks;
     if (wgs > 0x7fffffff) return fail(ATTS_ERR_SHAPE, "atts_gemm_nt_quant: the call has more than 2^31 workgroups");
-    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * p.waves), 0, stream, a); };
-    if (p.mt == 2) run(quant_kernel<T, G, 4, sizeof(T) == 2 ? 2 : 1, 4>);
-    else if (p.ns == 4) run(quant_kernel<T, G, 4, 1, 4>);
-    else run(p.ns == 2 ? quant_kernel<T, G, 2, 1, 8> : quant_kernel<T, G, 1, 1, 8>);
+    a.stage_steps = L::steps(p.steps_per_split);
+    const int32_t rc = allow_dynamic_lds<quant_kernel<T, G, NS, MT, W>>(L::bytes(L::kMost));
+    if (rc != ATTS_OK) return rc;
+    hipLaunchKernelGGL((quant_kernel<T, G, NS, MT, W>), dim3((unsigned)wgs), dim3(64 * W), L::bytes(a.stage_steps), stream, a);
     ATTS_LAUNCH_CHECK("quant_kernel");
     if (p.splits > 1) {
         hipLaunchKernelGGL(quant_join_kernel<T>, dim3((unsigned)ceil_div((int64_t)a.M * a.N, 256)), dim3(256), 0, stream, a);
@@ -366,9 +383,16 @@ int32_t launch_quant(const QuantPlan& p, const QuantArgs& a, hipStream_t stream)
     return ATTS_OK;
 }
 
+template <typename T, int G>
+int32_t launch_quant_shape(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
+    if (p.mt == 2) return launch_quant<T, G, 4, sizeof(T) == 2 ? 2 : 1, 4>(p, a, stream);
+    if (p.ns == 4) return launch_quant<T, G, 4, 1, 4>(p, a, stream);
+    return p.ns == 2 ? launch_quant<T, G, 2, 1, 8>(p, a, stream) : launch_quant<T, G, 1, 1, 8>(p, a, stream);
+}
+
 template <typename T>
 int32_t launch_quant_group(int32_t group, const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
-    return group == 32 ? launch_quant<T, 32>(p, a, stream) : group == 64 ? launch_quant<T, 64>(p, a, stream) : launch_quant<T, 128>(p, a, stream);
+    return group == 32 ? launch_quant_shape<T, 32>(p, a, stream) : group == 64 ? launch_quant_shape<T, 64>(p, a, stream) : launch_quant_shape<T, 128>(p, a, stream);
 }
 
 // Eight lanes a group: each holds group / 8 of its values, their limits are joined by three exchanges.
@@ -446,7 +470,7 @@ int32_t atts_gemm_nt_quant(int32_t dtype, const void* x, int64_t x_stride, const
     if (p.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.bytes))
         return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, p.bytes);
     const QuantArgs a{x, codes, scales, zeros, residual, out, static_cast<float*>(workspace), x_stride, M, N, Kdim, Kdim / group, epilogue,
-                      epilogue == ATTS_EPILOGUE_SWIGLU ? 2 * N : N, p.splits, p.steps_per_split, p.steps, p.row_blocks, p.tiles};
+                      epilogue == ATTS_EPILOGUE_SWIGLU ? 2 * N : N, p.splits, p.steps_per_split, p.steps, p.row_blocks, p.tiles, 0};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return dtype == ATTS_DTYPE_F32 ? launch_quant_group<float>(group, p, a, stream) : launch_quant_group<bf16>(group, p, a, stream);
 }
