@@ -1,0 +1,43 @@
+// Reductions over the lanes of a wavefront that never leave the vector registers.
+#pragma once
+
+#include "common.h"
+
+namespace atts {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true);
+}
+
+// Over the four lanes l % 16 + 16 c.
+template <typename F>
+__device__ __forceinline__ uint32_t across_rows(uint32_t x, F&& f) {
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = f(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return f(b[0], b[1]);
+}
+
+// Over all 64 lanes; f is commutative, and every lane takes the same steps on the same values.
+template <typename F>
+__device__ __forceinline__ uint32_t across_wave(uint32_t x, F&& f) {
+    x = f(x, dpp<0xB1>(x));       // lane ^ 1
+    x = f(x, dpp<0x4E>(x));       // lane ^ 2
+    x = f(x, dpp<0x141>(x));      // mirrored within eight: the other four
+    x = f(x, dpp<0x140>(x));      // mirrored within sixteen: the other eight
+    return across_rows(x, f);
+}
+
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+__device__ __forceinline__ uint32_t sum_bits(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
+
+__device__ __forceinline__ float row_max(float x) { return __uint_as_float(across_rows(__float_as_uint(x), max_bits)); }
+__device__ __forceinline__ float row_sum(float x) { return __uint_as_float(across_rows(__float_as_uint(x), sum_bits)); }
+__device__ __forceinline__ float wave_max(float x) { return __uint_as_float(across_wave(__float_as_uint(x), max_bits)); }
+__device__ __forceinline__ float wave_sum(float x) { return __uint_as_float(across_wave(__float_as_uint(x), sum_bits)); }
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) {
+    return across_wave(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+}  // namespace atts

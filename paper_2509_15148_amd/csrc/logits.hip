@@ -2,18 +2,24 @@
 // with the first arg max and the log-sum-exp of the result.
 //
 //   * A workgroup takes a slice of the vocabulary for the rows of one sequence.  How often each token of the slice came before is
-//     counted into LDS from the history (integer atomics: the order does not matter), once for all rows; a row adds the tokens
-//     of its own path before its turn and takes them out behind it.  Nothing of the size of the vocabulary is kept between calls.
-//   * The results stay in registers for the maximum and the sum of exponentials: one read and one write of the logits.  Every wavefront
-//     leaves (maximum, its index, sum) of its part; a second launch joins the parts of a row in a fixed order.
+//     counted into LDS from the history (integer atomics: the order does not matter), once for all rows.  The tokens of a row's own path in the tree are
+//     counted before its turn and taken out behind it, which for nearly all rows and slices is nothing at all.  Nothing of the size of
+//     the vocabulary is kept between calls.
+//   * The logits of the next row are requested before those of this one are used; results stay in registers for the maximum and the sum of
+//     exponentials: one read and one write of the logits.  Every wavefront leaves (maximum, its index, sum) of its part; a second launch joins the
+//     parts of a row in a fixed order.
+//   * Slices of 4096 tokens fill the chip with few rows; slices of 16,384 read a long history a quarter as often (logits_plan).
+#include "lanes.h"
 #include "paged.h"
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace atts {
 namespace {
 
-constexpr int kThreads = 256, kTokens = 16, kSlice = kThreads * kTokens, kWaves = kThreads / 64;
+constexpr int kTokens = 16;      // of a thread
 
 struct Part {
     float top, sum;          // maximum, sum of exp(x - top); top = -inf: nothing above -inf
@@ -28,10 +34,10 @@ struct LogitsArgs {
     const uint32_t* mask;
     Part* parts;
     int64_t in_stride, out_stride, mask_words;
-    int32_t max_rows, n_history, n_bias, R, V, slices, rows_per_wg;
+    int32_t max_rows, n_history, n_bias, R, V, n_parts, rows_per_wg;
 };
 
-// (top, id, sum) of two parts together; of equal maxima the lower index
+// (top, id, sum) of two parts together; of equal maxima the lower index.  Maxima are no NaNs.
 __device__ __forceinline__ void join(Part& a, float top, int id, float sum) {
     if (top > a.top) {
         a.sum = (a.top > -INFINITY ? a.sum * __expf(a.top - top) : a.sum) + sum;
@@ -43,45 +49,126 @@ __device__ __forceinline__ void join(Part& a, float top, int id, float sum) {
     }
 }
 
-// Steps 1 to 3 on one value.  Every operation is rounded by itself: no products are contracted into sums.
-__device__ __forceinline__ float adjust(float x, uint32_t word, const float4& p) {
+// Steps 1 to 3 on one value whose token came before.  Every operation is rounded by itself: no products are contracted into sums.
+__device__ __forceinline__ float penalise(float x, uint32_t word, const float4& p) {
 #pragma clang fp contract(off)
     const uint32_t count = word & 0x7fffffffu;
-    if (word) x = x > 0.f ? x / p.x : x * p.x;
+    x = x > 0.f ? x / p.x : x * p.x;
     x = x - (float)count * p.y;
     if (count) x = x - p.z;
     return x;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void logits_kernel(const T* __restrict__ logits, T* __restrict__ out, LogitsArgs a) {
-    __shared__ uint32_t seen[kSlice];                    // generated count; bit 31: in the prompt
-    __shared__ int32_t bias_at[kSlice];                  // 1 + position of the token's last bias entry, 0: none
-    __shared__ int16_t parent[ATTS_MAX_TREE];
+// x / t, correctly rounded, by the rounded reciprocal r of t: the quotient's error, exact by a fused multiply-add, corrects it once.  That
+// holds while nothing over- or underflows on the way (by_reciprocal); others are divided.
+template <int VEC>
+__device__ __forceinline__ void divide(float (&x)[VEC], float t, float r, bool by_reciprocal) {
+    float least = fabsf(x[0]), most = least;                // NaNs drop out of both: a NaN stays one either way
+#pragma unroll
+    for (int j = 1; j < VEC; ++j) {
+        least = fminf(least, fabsf(x[j]));
+        most = fmaxf(most, fabsf(x[j]));
+    }
+    if (by_reciprocal && least > 0x1p-60f && most < 0x1p60f) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float q = x[j] * r;
+            x[j] = fmaf(fmaf(-q, t, x[j]), r, q);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = x[j] / t;
+    }
+}
+
+template <typename T, int VEC> struct Load {
+    typedef T Raw __attribute__((ext_vector_type(VEC)));
+};
+template <typename T> struct Load<T, 1> {
+    typedef T Raw;
+};
+template <typename T, int VEC>
+__device__ __forceinline__ T element(const typename Load<T, VEC>::Raw& v, int i) {
+    if constexpr (VEC == 1) return v;
+    else return v[i];
+}
+
+// VEC consecutive tokens at a time (16 bytes), or 1 where addresses or V do not allow it.
+template <typename T, int VEC, int THREADS>
+__global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out, const LogitsArgs a) {
+    constexpr int kSlice = THREADS * kTokens, kLoads = kTokens / VEC;
+    typedef typename Load<T, VEC>::Raw Raw;
+    extern __shared__ __attribute__((aligned(16))) uint32_t smem[];
+    uint32_t* const seen = smem;                         // [kSlice] generated count; bit 31: in the prompt
+    int32_t* const bias_at = reinterpret_cast<int32_t*>(smem) + (a.params ? kSlice : 0);         // [kSlice] 1 + position of the token's last bias entry, 0: none
+    __shared__ int16_t parent[ATTS_MAX_TREE], nearest[ATTS_MAX_TREE];       // nearest: the first row on the way up, itself included, with a token of the slice
+    __shared__ int32_t token[ATTS_MAX_TREE];             // of a row of the tree, inside the slice, or -1
     const int tid = threadIdx.x, seq = blockIdx.z, v0 = blockIdx.x * kSlice, n_here = min(kSlice, a.V - v0);
     const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.R);
     if (first < 0) return;
     const int n = min(end - first, a.max_rows), r0 = blockIdx.y * a.rows_per_wg, r1 = min(r0 + a.rows_per_wg, n);
     if (r0 >= r1) return;
-    for (int i = tid; i < kSlice; i += kThreads) {
-        seen[i] = 0;
-        bias_at[i] = 0;
-    }
-    const bool paths = a.params && a.tree_ids;
-    if (paths)
-        for (int i = tid; i < n; i += kThreads) {
-            const int up = a.parents[first + i];
-            parent[i] = (int16_t)(up >= 0 && up < i ? up : -1);
+
+    // A row's logits and mask words; tokens behind the last one are read as it (a piece, where VEC > 1: VEC divides V then), and shut.
+    struct Row {
+        Raw x[kLoads];
+        uint32_t open[kLoads];
+    };
+    int at[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) at[i] = min((i * THREADS + tid) * VEC, n_here - VEC);
+    auto load = [&](Row& f, int row) __attribute__((always_inline)) {
+        const T* src = logits + (int64_t)(first + row) * a.in_stride + v0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) f.x[i] = *reinterpret_cast<const Raw*>(src + at[i]);
+        if (a.mask) {
+            const uint32_t* words = a.mask + (int64_t)(first + row) * a.mask_words;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) f.open[i] = words[(uint32_t)(v0 + at[i]) >> 5];
         }
-    __syncthreads();
+    };
+    Row now, next;
+    load(now, r0);
+
+    const bool paths = a.params && a.tree_ids;
+    if (a.params || a.bias_ids) {
+        const int words = (a.params ? kSlice : 0) + (a.bias_ids ? kSlice : 0);
+        for (int i = tid; i < words / 4; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+        if (paths)
+            for (int i = tid; i < n; i += THREADS) {
+                const int up = a.parents[first + i], v = a.tree_ids[first + i] - v0;
+                parent[i] = (int16_t)(up >= 0 && up < i ? up : -1);
+                token[i] = (uint32_t)v < (uint32_t)n_here ? v : -1;
+            }
+        __syncthreads();
+    }
     if (a.params && a.history) {
         const int h0 = min(max(a.history_offsets[seq], 0), a.n_history), h1 = min(max(a.history_offsets[seq + 1], h0), a.n_history);
         const int64_t split = (int64_t)h0 + (a.prompt_lens ? a.prompt_lens[seq] : 0);
-        for (int i = h0 + tid; i < h1; i += kThreads) {
-            const int v = a.history[i] - v0;
+        auto count = [&](int i, int id) __attribute__((always_inline)) {
+            const int v = id - v0;
             if ((uint32_t)v < (uint32_t)n_here) {
                 if (i < split) atomicOr(&seen[v], 0x80000000u);
                 else atomicAdd(&seen[v], 1u);
+            }
+        };
+        // in fours where they are aligned, eight of those at a time
+        const int lead = (int)((16 - ((uintptr_t)(a.history + h0) & 15)) & 15) / 4, q0 = min(h0 + lead, h1), quads = (h1 - q0) / 4;
+        if (tid < q0 - h0) count(h0 + tid, a.history[h0 + tid]);
+        if (tid < h1 - q0 - 4 * quads) count(q0 + 4 * quads + tid, a.history[q0 + 4 * quads + tid]);
+        const int4* const src = reinterpret_cast<const int4*>(a.history + q0);
+        for (int g = tid; g < quads; g += 8 * THREADS) {
+            int4 ids[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) ids[u] = src[min(g + u * THREADS, quads - 1)];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (g + u * THREADS >= quads) break;
+                const int i = q0 + 4 * (g + u * THREADS);
+                count(i, ids[u].x);
+                count(i + 1, ids[u].y);
+                count(i + 2, ids[u].z);
+                count(i + 3, ids[u].w);
             }
         }
     }
@@ -89,67 +176,96 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(const T* __restrict__ 
     if (a.bias_ids) {
         bias0 = min(max(a.bias_offsets[seq], 0), a.n_bias);
         const int b1 = min(max(a.bias_offsets[seq + 1], bias0), a.n_bias);
-        for (int i = bias0 + tid; i < b1; i += kThreads) {
+        for (int i = bias0 + tid; i < b1; i += THREADS) {
             const int v = a.bias_ids[i] - v0;
             if ((uint32_t)v < (uint32_t)n_here) atomicMax(&bias_at[v], i - bias0 + 1);
         }
     }
+    if (paths && tid < n) {                                // THREADS >= ATTS_MAX_TREE: a thread walks up from its own row
+        int up = tid;
+        while (up >= 0 && token[up] < 0) up = parent[up];
+        nearest[tid] = (int16_t)up;
+    }
+    __syncthreads();
     const float4 p = a.params ? reinterpret_cast<const float4*>(a.params)[seq] : make_float4(1.f, 0.f, 0.f, 1.f);
-    auto path = [&](int row, uint32_t step) {              // the tokens of the row's path, counted (step 1) or taken out again (-1)
-        if (tid == 0)
-            for (int at = row; at >= 0; at = parent[at]) {
-                const int v = a.tree_ids[first + at] - v0;
-                if ((uint32_t)v < (uint32_t)n_here) seen[v] += step;
-            }
+    const float by = 1.f / p.w;
+    const bool by_reciprocal = p.w > 0x1p-60f && p.w < 0x1p60f, scaled = p.w != 1.f;
+    // The tokens of the row's path, counted (step 1) or taken out again (-1), each by the thread that alone reads its count: no barrier.
+    auto count_path = [&](int row, uint32_t step) {
+        for (int up = nearest[row]; up >= 0; up = parent[up] >= 0 ? nearest[parent[up]] : -1) {
+            const int t = token[up];
+            if (t / VEC % THREADS == tid) seen[t] += step;
+        }
     };
+
     for (int row = r0; row < r1; ++row) {
         const int64_t r = first + row;
-        __syncthreads();
-        if (paths) {
-            path(row, 1u);
-            __syncthreads();
-        }
-        const T* src = logits + r * a.in_stride + v0;
-        T* dst = out + r * a.out_stride + v0;
+        load(next, min(row + 1, r1 - 1));
+        if (paths) count_path(row, 1u);
+        T* const dst = out + r * a.out_stride + v0;
         float x[kTokens], top = -INFINITY;
-        int id = -1;
 #pragma unroll
-        for (int i = 0; i < kTokens; ++i) {
-            const int t = i * kThreads + tid;
-            x[i] = -INFINITY;
-            if (t < n_here) {
-                float y = to_f32(src[t]);
-                if (a.params) y = adjust(y, seen[t], p);
-                if (a.bias_ids && bias_at[t]) y = y + a.bias_values[bias0 + bias_at[t] - 1];
-                if (a.params) y = y / p.w;
-                if (a.mask) {
-                    const uint32_t v = (uint32_t)(v0 + t);
-                    if (!(a.mask[r * a.mask_words + (v >> 5)] >> (v & 31) & 1)) y = -INFINITY;
+        for (int i = 0; i < kLoads; ++i) {
+            const bool live = (i * THREADS + tid) * VEC < n_here;
+            float z[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) z[j] = to_f32(element<T, VEC>(now.x[i], j));
+            if (a.params) {
+                uint32_t word[VEC], any = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) any |= word[j] = seen[at[i] + j];
+                if (any) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (word[j]) z[j] = penalise(z[j], word[j], p);
                 }
-                dst[t] = from_f32<T>(y);
-                x[i] = y;
-                if (y > top) { top = y; id = v0 + t; }
             }
+            if (a.bias_ids) {
+                int entry[VEC], any = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) any |= entry[j] = bias_at[at[i] + j];
+                if (any) {
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (entry[j]) z[j] = z[j] + a.bias_values[bias0 + entry[j] - 1];
+                }
+            }
+            if (scaled) divide<VEC>(z, p.w, by, by_reciprocal);
+            // bit j of `open`: token j is allowed; VEC divides 32, so one word holds them
+            const uint32_t open = !live ? 0u : a.mask ? now.open[i] >> ((v0 + at[i]) & 31) : ~0u;
+            Raw y = {};
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const uint32_t keep = (uint32_t)((int32_t)(open << (31 - j)) >> 31);
+                const float shut = __uint_as_float((__float_as_uint(z[j]) & keep) | (0xff800000u & ~keep));
+                x[i * VEC + j] = shut;
+                top = fmaxf(top, shut);
+                if constexpr (VEC == 1) y = from_f32<T>(shut);
+                else y[j] = from_f32<T>(shut);
+            }
+            if (live) *reinterpret_cast<Raw*>(dst + at[i]) = y;
         }
+        if (paths) count_path(row, ~0u);
         if (a.parts) {
-            float best = top;
-#pragma unroll
-            for (int d = 32; d; d >>= 1) best = fmaxf(best, __shfl_xor(best, d, 64));
-            int lowest = top == best && id >= 0 ? id : 0x7fffffff;
-#pragma unroll
-            for (int d = 32; d; d >>= 1) lowest = min(lowest, __shfl_xor(lowest, d, 64));
+            const float best = wave_max(top);
             float sum = 0.f;
+            if (fabsf(best) < INFINITY) {
 #pragma unroll
-            for (int i = 0; i < kTokens; ++i) sum += best > -INFINITY ? x[i] == best ? 1.f : __expf(x[i] - best) : isnan(x[i]) ? x[i] : 0.f;
+                for (int i = 0; i < kTokens; ++i) sum += __builtin_amdgcn_exp2f((x[i] - best) * 1.4426950408889634f);
+            } else {                                        // nothing above -inf, or +inf: NaNs stay NaN, the others count if they are the maximum +inf
 #pragma unroll
-            for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-            if ((tid & 63) == 0)
-                a.parts[(r * a.slices + blockIdx.x) * kWaves + (tid >> 6)] = Part{best, sum, lowest == 0x7fffffff ? -1 : lowest, 0};
+                for (int i = 0; i < kTokens; ++i) sum += isnan(x[i]) ? x[i] : x[i] == INFINITY ? 1.f : 0.f;
+            }
+            sum = wave_sum(sum);
+            uint32_t lowest = ~0u;
+            if (top == best && best > -INFINITY) {
+#pragma unroll
+                for (int i = kTokens - 1; i >= 0; --i) lowest = x[i] == best ? (uint32_t)(v0 + at[i / VEC] + i % VEC) : lowest;
+            }
+            lowest = wave_min(lowest);
+            if ((tid & 63) == 0) a.parts[r * a.n_parts + blockIdx.x * (THREADS / 64) + (tid >> 6)] = Part{best, sum, (int32_t)lowest, 0};
         }
-        if (paths) {
-            __syncthreads();
-            path(row, ~0u);
-        }
+        now = next;
     }
 }
 
@@ -175,7 +291,38 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const Part* __restrict_
     if (lse) lse[r] = p.top > -INFINITY ? p.top + __logf(p.sum) : isnan(p.sum) ? p.sum : -INFINITY;
 }
 
-int64_t slices_of(int32_t V) { return ceil_div(V, kSlice); }
+// Threads of a workgroup, slices of the vocabulary and rows of a workgroup.
+struct LogitsPlan {
+    int32_t threads, slices, rows_per_wg;
+};
+
+LogitsPlan logits_plan(int32_t n_seqs, int32_t max_rows, int32_t V) {
+    LogitsPlan p;
+    p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 ? 1024 : 256;
+    p.slices = (int32_t)ceil_div(V, p.threads * kTokens);
+    const int64_t cells = (int64_t)n_seqs * p.slices, chunks = std::min<int64_t>(max_rows, std::max<int64_t>(1, 1536 / std::max<int64_t>(1, cells)));
+    p.rows_per_wg = (int32_t)ceil_div(max_rows, chunks);
+    return p;
+}
+
+template <typename T>
+int32_t launch_logits(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
+    constexpr int kVec = 16 / sizeof(T);
+    const bool vec = !(((uintptr_t)logits | (uintptr_t)out) & 15) && a.V % kVec == 0 && a.in_stride % kVec == 0 && a.out_stride % kVec == 0;
+    const dim3 grid((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs);
+    const size_t table = (size_t)p.threads * kTokens * 4, lds = (a.params ? table : 0) + (a.bias_ids ? table : 0);
+    const auto run = [&](auto kernel, int32_t allowed) {
+        if (allowed != ATTS_OK) return allowed;
+        hipLaunchKernelGGL(kernel, grid, dim3(p.threads), lds, stream, static_cast<const T*>(logits), static_cast<T*>(out), a);
+        ATTS_LAUNCH_CHECK("logits_kernel");
+        return (int32_t)ATTS_OK;
+    };
+    constexpr size_t most = 2 * 1024 * kTokens * 4;
+    if (p.threads == 1024)
+        return vec ? run(logits_kernel<T, kVec, 1024>, allow_dynamic_lds<logits_kernel<T, kVec, 1024>>(most))
+                   : run(logits_kernel<T, 1, 1024>, allow_dynamic_lds<logits_kernel<T, 1, 1024>>(most));
+    return vec ? run(logits_kernel<T, kVec, 256>, ATTS_OK) : run(logits_kernel<T, 1, 256>, ATTS_OK);
+}
 
 }  // namespace
 }  // namespace atts
@@ -188,7 +335,7 @@ int32_t atts_logits_adjust_workspace_bytes(int32_t R, int32_t V, size_t* out_byt
     const char* fn = "atts_logits_adjust_workspace_bytes";
     if (!out_bytes) return fail(ATTS_ERR_INVALID_ARG, "%s: out_bytes is NULL", fn);
     if (R < 0 || R > (1 << 24) || V < 1 || V > (1 << 30)) return fail(ATTS_ERR_INVALID_ARG, "%s: R outside [0, 2^24] or V outside [1, 2^30]", fn);
-    *out_bytes = align_up((size_t)R * slices_of(V) * kWaves * sizeof(Part), 256);
+    *out_bytes = align_up((size_t)R * ceil_div(V, 1024 * kTokens) * 16 * sizeof(Part), 256);      // a part for every wavefront, whichever the slices
     return ATTS_OK;
 }
 
@@ -215,18 +362,16 @@ int32_t atts_logits_adjust(int32_t dtype, const void* logits, int64_t logits_str
     const bool decide = top_ids || lse;
     if (decide && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need))
         return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, need);
-    LogitsArgs a{row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_offsets, bias_values, mask,
-                 decide ? static_cast<Part*>(workspace) : nullptr, logits_stride, out_stride, ceil_div(V, 32), max_rows, n_history, n_bias, R, V,
-                 (int32_t)slices_of(V), max_rows};
+    const LogitsPlan p = logits_plan(n_seqs, max_rows, V);
+    const LogitsArgs a{row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_offsets, bias_values, mask,
+                       decide ? static_cast<Part*>(workspace) : nullptr, logits_stride, out_stride, ceil_div(V, 32), max_rows, n_history, n_bias, R, V,
+                       p.slices * (p.threads / 64), p.rows_per_wg};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const dim3 grid((unsigned)a.slices, (unsigned)ceil_div(max_rows, a.rows_per_wg), (unsigned)n_seqs);
-    if (dtype == ATTS_DTYPE_F32)
-        hipLaunchKernelGGL(logits_kernel<float>, grid, dim3(kThreads), 0, stream, static_cast<const float*>(logits), static_cast<float*>(out), a);
-    else
-        hipLaunchKernelGGL(logits_kernel<bf16>, grid, dim3(kThreads), 0, stream, static_cast<const bf16*>(logits), static_cast<bf16*>(out), a);
-    ATTS_LAUNCH_CHECK("logits_kernel");
+    const int32_t launched = dtype == ATTS_DTYPE_F32 ? launch_logits<float>(p, a, n_seqs, logits, out, stream)
+                                                     : launch_logits<bf16>(p, a, n_seqs, logits, out, stream);
+    if (launched != ATTS_OK) return launched;
     if (decide) {
-        hipLaunchKernelGGL(logits_join_kernel, dim3((unsigned)R), dim3(64), 0, stream, a.parts, row_offsets, n_seqs, max_rows, a.slices * kWaves, top_ids, lse);
+        hipLaunchKernelGGL(logits_join_kernel, dim3((unsigned)R), dim3(64), 0, stream, a.parts, row_offsets, n_seqs, max_rows, a.n_parts, top_ids, lse);
         ATTS_LAUNCH_CHECK("logits_join_kernel");
     }
     return ATTS_OK;
