@@ -49,35 +49,51 @@ __device__ __forceinline__ void join(Part& a, float top, int id, float sum) {
     }
 }
 
-// Steps 1 to 3 on one value whose token came before.  Every operation is rounded by itself: no products are contracted into sums.
-__device__ __forceinline__ float penalise(float x, uint32_t word, const float4& p) {
-#pragma clang fp contract(off)
-    const uint32_t count = word & 0x7fffffffu;
-    x = x > 0.f ? x / p.x : x * p.x;
-    x = x - (float)count * p.y;
-    if (count) x = x - p.z;
-    return x;
-}
-
-// x / t, correctly rounded, by the rounded reciprocal r of t: the quotient's error, exact by a fused multiply-add, corrects it once.  That
-// holds while nothing over- or underflows on the way (by_reciprocal); others are divided.
+// A divisor t and its rounded reciprocal.  x / t comes out correctly rounded from x times it: the quotient's error, exact by a fused
+// multiply-add, corrects it once.  That holds while nothing over- or underflows on the way (within); other values are divided.
+struct Divisor {
+    float t, r;
+    bool usual;
+    __device__ explicit Divisor(float by) : t(by), r(1.f / by), usual(by > 0x1p-60f && by < 0x1p60f) {}
+    __device__ __forceinline__ float quotient(float x) const {
+        const float q = x * r;
+        return fmaf(fmaf(-q, t, x), r, q);
+    }
+};
 template <int VEC>
-__device__ __forceinline__ void divide(float (&x)[VEC], float t, float r, bool by_reciprocal) {
-    float least = fabsf(x[0]), most = least;                // NaNs drop out of both: a NaN stays one either way
+__device__ __forceinline__ bool within(const float (&x)[VEC]) {      // NaNs drop out: a NaN stays one either way
+    float least = fabsf(x[0]), most = least;
 #pragma unroll
     for (int j = 1; j < VEC; ++j) {
         least = fminf(least, fabsf(x[j]));
         most = fmaxf(most, fabsf(x[j]));
     }
-    if (by_reciprocal && least > 0x1p-60f && most < 0x1p60f) {
+    return least > 0x1p-60f && most < 0x1p60f;
+}
+
+// Steps 1 to 3 on VEC values with what is known of their tokens.  Every operation is rounded by itself: no products are contracted into sums.
+template <int VEC>
+__device__ __forceinline__ void penalise(float (&x)[VEC], const uint32_t (&word)[VEC], uint32_t generated, const Divisor& repetition, float frequency,
+                                         float presence) {
+#pragma clang fp contract(off)
+    if (repetition.usual && within<VEC>(x)) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const float q = x[j] * r;
-            x[j] = fmaf(fmaf(-q, t, x[j]), r, q);
+            const uint32_t count = word[j] & generated;
+            float y = x[j] > 0.f ? repetition.quotient(x[j]) : x[j] * repetition.t;
+            y = y - (float)count * frequency;
+            y = count ? y - presence : y;
+            x[j] = word[j] ? y : x[j];
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = x[j] / t;
+        for (int j = 0; j < VEC; ++j)
+            if (word[j]) {
+                const uint32_t count = word[j] & generated;
+                float y = x[j] > 0.f ? x[j] / repetition.t : x[j] * repetition.t;
+                y = y - (float)count * frequency;
+                x[j] = count ? y - presence : y;
+            }
     }
 }
 
@@ -93,17 +109,19 @@ __device__ __forceinline__ T element(const typename Load<T, VEC>::Raw& v, int i)
     else return v[i];
 }
 
-// VEC consecutive tokens at a time (16 bytes), or 1 where addresses or V do not allow it.
-template <typename T, int VEC, int THREADS>
-__global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out, const LogitsArgs a) {
-    constexpr int kSlice = THREADS * kTokens, kLoads = kTokens / VEC;
+// VEC consecutive tokens at a time (16 bytes), or 1 where addresses or V do not allow it; a slice takes PASSES rounds of kTokens a thread.
+template <typename T, int VEC, int THREADS, int PASSES>
+__global__ __launch_bounds__(THREADS, 4) void logits_kernel(const T* logits, T* out, const LogitsArgs a) {
+    constexpr int kRound = THREADS * kTokens, kSlice = kRound * PASSES, kLoads = kTokens / VEC;
     typedef typename Load<T, VEC>::Raw Raw;
     extern __shared__ __attribute__((aligned(16))) uint32_t smem[];
-    uint32_t* const seen = smem;                         // [kSlice] generated count; bit 31: in the prompt
-    int32_t* const bias_at = reinterpret_cast<int32_t*>(smem) + (a.params ? kSlice : 0);         // [kSlice] 1 + position of the token's last bias entry, 0: none
+    uint32_t* const seen = smem;                         // [kSlice + 64] how often a token came before, none: 0
+    int32_t* const bias_at = reinterpret_cast<int32_t*>(smem) + (a.params ? kSlice + 64 : 0);    // [kSlice] 1 + position of the token's last bias entry, 0: none
     __shared__ int16_t parent[ATTS_MAX_TREE], nearest[ATTS_MAX_TREE];       // nearest: the first row on the way up, itself included, with a token of the slice
     __shared__ int32_t token[ATTS_MAX_TREE];             // of a row of the tree, inside the slice, or -1
-    const int tid = threadIdx.x, seq = blockIdx.z, v0 = blockIdx.x * kSlice, n_here = min(kSlice, a.V - v0);
+    // Common words have low ids, so the first slice counts most of a history: sequences begin with different slices, or all of the first ones
+    // would share an XCD.
+    const int tid = threadIdx.x, seq = blockIdx.z, slice = (blockIdx.x + seq) % gridDim.x, v0 = slice * kSlice, n_here = min(kSlice, a.V - v0);
     const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.R);
     if (first < 0) return;
     const int n = min(end - first, a.max_rows), r0 = blockIdx.y * a.rows_per_wg, r1 = min(r0 + a.rows_per_wg, n);
@@ -114,25 +132,25 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out
         Raw x[kLoads];
         uint32_t open[kLoads];
     };
-    int at[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) at[i] = min((i * THREADS + tid) * VEC, n_here - VEC);
-    auto load = [&](Row& f, int row) __attribute__((always_inline)) {
+    // item: row and round, rounds of a row one behind the other
+    const auto place = [&](int round, int i) { return max(min(round * kRound + (i * THREADS + tid) * VEC, n_here - VEC), 0); };
+    auto load = [&](Row& f, int item) __attribute__((always_inline)) {
+        const int row = r0 + item / PASSES, round = item % PASSES;
         const T* src = logits + (int64_t)(first + row) * a.in_stride + v0;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) f.x[i] = *reinterpret_cast<const Raw*>(src + at[i]);
+        for (int i = 0; i < kLoads; ++i) f.x[i] = *reinterpret_cast<const Raw*>(src + place(round, i));
         if (a.mask) {
             const uint32_t* words = a.mask + (int64_t)(first + row) * a.mask_words;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) f.open[i] = words[(uint32_t)(v0 + at[i]) >> 5];
+            for (int i = 0; i < kLoads; ++i) f.open[i] = words[(uint32_t)(v0 + place(round, i)) >> 5];
         }
     };
     Row now, next;
-    load(now, r0);
+    load(now, 0);
 
     const bool paths = a.params && a.tree_ids;
     if (a.params || a.bias_ids) {
-        const int words = (a.params ? kSlice : 0) + (a.bias_ids ? kSlice : 0);
+        const int words = (a.params ? kSlice + 64 : 0) + (a.bias_ids ? kSlice : 0);
         for (int i = tid; i < words / 4; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
         if (paths)
             for (int i = tid; i < n; i += THREADS) {
@@ -142,34 +160,46 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out
             }
         __syncthreads();
     }
+    uint32_t generated = 0x7fffffffu;                     // bits of a word that count what was generated; the others: in the prompt
     if (a.params && a.history) {
         const int h0 = min(max(a.history_offsets[seq], 0), a.n_history), h1 = min(max(a.history_offsets[seq + 1], h0), a.n_history);
-        const int64_t split = (int64_t)h0 + (a.prompt_lens ? a.prompt_lens[seq] : 0);
-        auto count = [&](int i, int id) __attribute__((always_inline)) {
-            const int v = id - v0;
-            if ((uint32_t)v < (uint32_t)n_here) {
-                if (i < split) atomicOr(&seen[v], 0x80000000u);
-                else atomicAdd(&seen[v], 1u);
+        const int split = h0 + min(max(a.prompt_lens ? a.prompt_lens[seq] : 0, 0), h1 - h0);
+        // Words of a history that is short enough hold 16 bits for the prompt and 16 for what was generated, so that an entry is one addition
+        // without a branch; entries of other slices go to a word of their lane's own behind the table.
+        const auto scan = [&](auto count) __attribute__((always_inline)) {
+            // in fours where they are aligned, four of those at a time
+            const int lead = (int)((16 - ((uintptr_t)(a.history + h0) & 15)) & 15) / 4, q0 = min(h0 + lead, h1), quads = (h1 - q0) / 4;
+            if (tid < q0 - h0) count(h0 + tid, a.history[h0 + tid]);
+            if (tid < h1 - q0 - 4 * quads) count(q0 + 4 * quads + tid, a.history[q0 + 4 * quads + tid]);
+            const int4* const src = reinterpret_cast<const int4*>(a.history + q0);
+            for (int g = tid; g < quads; g += 4 * THREADS) {
+                int4 ids[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) ids[u] = src[min(g + u * THREADS, quads - 1)];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = q0 + 4 * (g + u * THREADS), none = g + u * THREADS < quads ? 0 : -1;
+                    count(i, ids[u].x | none);
+                    count(i + 1, ids[u].y | none);
+                    count(i + 2, ids[u].z | none);
+                    count(i + 3, ids[u].w | none);
+                }
             }
         };
-        // in fours where they are aligned, eight of those at a time
-        const int lead = (int)((16 - ((uintptr_t)(a.history + h0) & 15)) & 15) / 4, q0 = min(h0 + lead, h1), quads = (h1 - q0) / 4;
-        if (tid < q0 - h0) count(h0 + tid, a.history[h0 + tid]);
-        if (tid < h1 - q0 - 4 * quads) count(q0 + 4 * quads + tid, a.history[q0 + 4 * quads + tid]);
-        const int4* const src = reinterpret_cast<const int4*>(a.history + q0);
-        for (int g = tid; g < quads; g += 8 * THREADS) {
-            int4 ids[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) ids[u] = src[min(g + u * THREADS, quads - 1)];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (g + u * THREADS >= quads) break;
-                const int i = q0 + 4 * (g + u * THREADS);
-                count(i, ids[u].x);
-                count(i + 1, ids[u].y);
-                count(i + 2, ids[u].z);
-                count(i + 3, ids[u].w);
-            }
+        if (h1 - h0 < 65536 - ATTS_MAX_TREE) {
+            generated = 0xffffu;
+            scan([&](int i, int id) __attribute__((always_inline)) {
+                const uint32_t v = (uint32_t)id - (uint32_t)v0;
+                atomicAdd(&seen[v < (uint32_t)n_here ? v : kSlice + (tid & 63)], i < split ? 0x10000u : 1u);
+            });
+        } else {
+            scan([&](int i, int id) __attribute__((always_inline)) {
+                const uint32_t v = (uint32_t)id - (uint32_t)v0;
+                if (v < (uint32_t)n_here) {
+                    if (i < split) atomicOr(&seen[v], 0x80000000u);
+                    else atomicAdd(&seen[v], 1u);
+                }
+            });
         }
     }
     int bias0 = 0;
@@ -188,62 +218,66 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out
     }
     __syncthreads();
     const float4 p = a.params ? reinterpret_cast<const float4*>(a.params)[seq] : make_float4(1.f, 0.f, 0.f, 1.f);
-    const float by = 1.f / p.w;
-    const bool by_reciprocal = p.w > 0x1p-60f && p.w < 0x1p60f, scaled = p.w != 1.f;
+    const Divisor repetition(p.x), temperature(p.w);
+    const bool scaled = p.w != 1.f;
     // The tokens of the row's path, counted (step 1) or taken out again (-1), each by the thread that alone reads its count: no barrier.
     auto count_path = [&](int row, uint32_t step) {
         for (int up = nearest[row]; up >= 0; up = parent[up] >= 0 ? nearest[parent[up]] : -1) {
             const int t = token[up];
-            if (t / VEC % THREADS == tid) seen[t] += step;
+            if (t / VEC % THREADS == tid) seen[t] += step;      // kRound is a multiple of VEC THREADS: the same thread in every round
         }
     };
 
-    for (int row = r0; row < r1; ++row) {
+    const int items = (r1 - r0) * PASSES;
+    for (int item = 0; item < items; ++item) {
+        const int row = r0 + item / PASSES, round = item % PASSES;
         const int64_t r = first + row;
-        load(next, min(row + 1, r1 - 1));
+        load(next, min(item + 1, items - 1));
         if (paths) count_path(row, 1u);
         T* const dst = out + r * a.out_stride + v0;
-        float x[kTokens], top = -INFINITY;
+        float x[kTokens], most[kLoads], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const bool live = (i * THREADS + tid) * VEC < n_here;
+            const int at = place(round, i);
+            const bool live = round * kRound + (i * THREADS + tid) * VEC < n_here;
             float z[VEC];
 #pragma unroll
             for (int j = 0; j < VEC; ++j) z[j] = to_f32(element<T, VEC>(now.x[i], j));
             if (a.params) {
                 uint32_t word[VEC], any = 0;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) any |= word[j] = seen[at[i] + j];
-                if (any) {
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j)
-                        if (word[j]) z[j] = penalise(z[j], word[j], p);
-                }
+                for (int j = 0; j < VEC; ++j) any |= word[j] = seen[at + j];
+                if (any) penalise<VEC>(z, word, generated, repetition, p.y, p.z);
             }
             if (a.bias_ids) {
                 int entry[VEC], any = 0;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) any |= entry[j] = bias_at[at[i] + j];
+                for (int j = 0; j < VEC; ++j) any |= entry[j] = bias_at[at + j];
                 if (any) {
 #pragma unroll
                     for (int j = 0; j < VEC; ++j)
                         if (entry[j]) z[j] = z[j] + a.bias_values[bias0 + entry[j] - 1];
                 }
             }
-            if (scaled) divide<VEC>(z, p.w, by, by_reciprocal);
+            if (scaled) {
+                const bool plain = temperature.usual && within<VEC>(z);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) z[j] = plain ? temperature.quotient(z[j]) : z[j] / temperature.t;
+            }
             // bit j of `open`: token j is allowed; VEC divides 32, so one word holds them
-            const uint32_t open = !live ? 0u : a.mask ? now.open[i] >> ((v0 + at[i]) & 31) : ~0u;
+            const uint32_t open = !live ? 0u : a.mask ? now.open[i] >> ((v0 + at) & 31) : ~0u;
             Raw y = {};
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 const uint32_t keep = (uint32_t)((int32_t)(open << (31 - j)) >> 31);
                 const float shut = __uint_as_float((__float_as_uint(z[j]) & keep) | (0xff800000u & ~keep));
                 x[i * VEC + j] = shut;
-                top = fmaxf(top, shut);
+                most[i] = j ? fmaxf(most[i], shut) : fmaxf(shut, -INFINITY);
                 if constexpr (VEC == 1) y = from_f32<T>(shut);
                 else y[j] = from_f32<T>(shut);
             }
-            if (live) *reinterpret_cast<Raw*>(dst + at[i]) = y;
+            top = fmaxf(top, most[i]);
+            if (live) *reinterpret_cast<Raw*>(dst + at) = y;
         }
         if (paths) count_path(row, ~0u);
         if (a.parts) {
@@ -257,13 +291,17 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out
                 for (int i = 0; i < kTokens; ++i) sum += isnan(x[i]) ? x[i] : x[i] == INFINITY ? 1.f : 0.f;
             }
             sum = wave_sum(sum);
-            uint32_t lowest = ~0u;
-            if (top == best && best > -INFINITY) {
+            uint32_t lowest = ~0u;                          // the first piece that holds the maximum, in any lane, has its lowest index
+            bool found = !(best > -INFINITY);
 #pragma unroll
-                for (int i = kTokens - 1; i >= 0; --i) lowest = x[i] == best ? (uint32_t)(v0 + at[i / VEC] + i % VEC) : lowest;
-            }
+            for (int i = 0; i < kLoads; ++i)
+                if (!found && __ballot(most[i] == best) != 0) {
+                    found = true;
+#pragma unroll
+                    for (int j = VEC - 1; j >= 0; --j) lowest = x[i * VEC + j] == best ? (uint32_t)(v0 + place(round, i) + j) : lowest;
+                }
             lowest = wave_min(lowest);
-            if ((tid & 63) == 0) a.parts[r * a.n_parts + blockIdx.x * (THREADS / 64) + (tid >> 6)] = Part{best, sum, (int32_t)lowest, 0};
+            if ((tid & 63) == 0) a.parts[r * a.n_parts + (slice * PASSES + round) * (THREADS / 64) + (tid >> 6)] = Part{best, sum, (int32_t)lowest, 0};
         }
         now = next;
     }
@@ -273,7 +311,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(const T* logits, T* out
 __global__ __launch_bounds__(64) void logits_join_kernel(const Part* __restrict__ parts, const int32_t* __restrict__ row_offsets, int n_seqs, int max_rows,
                                                          int n_parts, int32_t* __restrict__ top_ids, float* __restrict__ lse) {
     const int r = blockIdx.x, lane = threadIdx.x;
-    const int seq = sequence_of(row_offsets, n_seqs, r);
+    const int seq = sequence_of_wave(row_offsets, n_seqs, r, lane);
     if (seq < 0 || r - row_offsets[seq] >= max_rows || row_offsets[seq] < 0) return;
     Part p{-INFINITY, 0.f, -1, 0};
     for (int i = lane; i < n_parts; i += 64) {
@@ -291,37 +329,44 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const Part* __restrict_
     if (lse) lse[r] = p.top > -INFINITY ? p.top + __logf(p.sum) : isnan(p.sum) ? p.sum : -INFINITY;
 }
 
-// Threads of a workgroup, slices of the vocabulary and rows of a workgroup.
+// Threads of a workgroup, rounds and slices of the vocabulary, rows of a workgroup.
 struct LogitsPlan {
-    int32_t threads, slices, rows_per_wg;
+    int32_t threads, passes, slices, rows_per_wg;
 };
 
-LogitsPlan logits_plan(int32_t n_seqs, int32_t max_rows, int32_t V) {
+LogitsPlan logits_plan(int32_t n_seqs, int32_t max_rows, int32_t V, bool counts, bool bias) {
     LogitsPlan p;
     p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 ? 1024 : 256;
-    p.slices = (int32_t)ceil_div(V, p.threads * kTokens);
+    p.passes = p.threads == 1024 && counts && !bias ? 2 : 1;                  // with biases too, two rounds' tables do not fit the LDS
+    p.slices = (int32_t)ceil_div(V, p.threads * kTokens * p.passes);
     const int64_t cells = (int64_t)n_seqs * p.slices, chunks = std::min<int64_t>(max_rows, std::max<int64_t>(1, 1536 / std::max<int64_t>(1, cells)));
     p.rows_per_wg = (int32_t)ceil_div(max_rows, chunks);
     return p;
 }
 
-template <typename T>
+template <typename T, int VEC, int THREADS, int PASSES>
 int32_t launch_logits(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
+    constexpr size_t table = (size_t)THREADS * kTokens * PASSES * 4;
+    constexpr bool both = 2 * table <= 160 * 1024 - 4096;
+    const int32_t rc = allow_dynamic_lds<logits_kernel<T, VEC, THREADS, PASSES>>((both ? 2 * table : table) + 256);
+    if (rc != ATTS_OK) return rc;
+    hipLaunchKernelGGL((logits_kernel<T, VEC, THREADS, PASSES>), dim3((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs),
+                       dim3(THREADS), (a.params ? table + 256 : 0) + (a.bias_ids ? table : 0), stream, static_cast<const T*>(logits), static_cast<T*>(out), a);
+    ATTS_LAUNCH_CHECK("logits_kernel");
+    return ATTS_OK;
+}
+
+template <typename T, int VEC>
+int32_t launch_logits_shape(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
+    if (p.threads == 256) return launch_logits<T, VEC, 256, 1>(p, a, n_seqs, logits, out, stream);
+    return p.passes == 2 ? launch_logits<T, VEC, 1024, 2>(p, a, n_seqs, logits, out, stream) : launch_logits<T, VEC, 1024, 1>(p, a, n_seqs, logits, out, stream);
+}
+
+template <typename T>
+int32_t launch_logits_type(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
     constexpr int kVec = 16 / sizeof(T);
     const bool vec = !(((uintptr_t)logits | (uintptr_t)out) & 15) && a.V % kVec == 0 && a.in_stride % kVec == 0 && a.out_stride % kVec == 0;
-    const dim3 grid((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs);
-    const size_t table = (size_t)p.threads * kTokens * 4, lds = (a.params ? table : 0) + (a.bias_ids ? table : 0);
-    const auto run = [&](auto kernel, int32_t allowed) {
-        if (allowed != ATTS_OK) return allowed;
-        hipLaunchKernelGGL(kernel, grid, dim3(p.threads), lds, stream, static_cast<const T*>(logits), static_cast<T*>(out), a);
-        ATTS_LAUNCH_CHECK("logits_kernel");
-        return (int32_t)ATTS_OK;
-    };
-    constexpr size_t most = 2 * 1024 * kTokens * 4;
-    if (p.threads == 1024)
-        return vec ? run(logits_kernel<T, kVec, 1024>, allow_dynamic_lds<logits_kernel<T, kVec, 1024>>(most))
-                   : run(logits_kernel<T, 1, 1024>, allow_dynamic_lds<logits_kernel<T, 1, 1024>>(most));
-    return vec ? run(logits_kernel<T, kVec, 256>, ATTS_OK) : run(logits_kernel<T, 1, 256>, ATTS_OK);
+    return vec ? launch_logits_shape<T, kVec>(p, a, n_seqs, logits, out, stream) : launch_logits_shape<T, 1>(p, a, n_seqs, logits, out, stream);
 }
 
 }  // namespace
@@ -335,7 +380,7 @@ int32_t atts_logits_adjust_workspace_bytes(int32_t R, int32_t V, size_t* out_byt
     const char* fn = "atts_logits_adjust_workspace_bytes";
     if (!out_bytes) return fail(ATTS_ERR_INVALID_ARG, "%s: out_bytes is NULL", fn);
     if (R < 0 || R > (1 << 24) || V < 1 || V > (1 << 30)) return fail(ATTS_ERR_INVALID_ARG, "%s: R outside [0, 2^24] or V outside [1, 2^30]", fn);
-    *out_bytes = align_up((size_t)R * ceil_div(V, 1024 * kTokens) * 16 * sizeof(Part), 256);      // a part for every wavefront, whichever the slices
+    *out_bytes = align_up((size_t)R * ceil_div(V, 2048 * kTokens) * 32 * sizeof(Part), 256);      // a part for every wavefront, whichever the slices
     return ATTS_OK;
 }
 
@@ -362,13 +407,13 @@ int32_t atts_logits_adjust(int32_t dtype, const void* logits, int64_t logits_str
     const bool decide = top_ids || lse;
     if (decide && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need))
         return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, need);
-    const LogitsPlan p = logits_plan(n_seqs, max_rows, V);
+    const LogitsPlan p = logits_plan(n_seqs, max_rows, V, params != nullptr, bias_ids != nullptr);
     const LogitsArgs a{row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_offsets, bias_values, mask,
                        decide ? static_cast<Part*>(workspace) : nullptr, logits_stride, out_stride, ceil_div(V, 32), max_rows, n_history, n_bias, R, V,
-                       p.slices * (p.threads / 64), p.rows_per_wg};
+                       p.slices * p.passes * (p.threads / 64), p.rows_per_wg};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const int32_t launched = dtype == ATTS_DTYPE_F32 ? launch_logits<float>(p, a, n_seqs, logits, out, stream)
-                                                     : launch_logits<bf16>(p, a, n_seqs, logits, out, stream);
+    const int32_t launched = dtype == ATTS_DTYPE_F32 ? launch_logits_type<float>(p, a, n_seqs, logits, out, stream)
+                                                     : launch_logits_type<bf16>(p, a, n_seqs, logits, out, stream);
     if (launched != ATTS_OK) return launched;
     if (decide) {
         hipLaunchKernelGGL(logits_join_kernel, dim3((unsigned)R), dim3(64), 0, stream, a.parts, row_offsets, n_seqs, max_rows, a.n_parts, top_ids, lse);

@@ -31,6 +31,22 @@ __device__ __forceinline__ int sequence_of(const int32_t* __restrict__ row_offse
     return lo;
 }
 
+// The same by a whole wavefront, 64 sequences a step: a search by halves waits for memory at every one of its steps.
+__device__ __forceinline__ int sequence_of_wave(const int32_t* __restrict__ row_offsets, int n_seqs, int r, int lane) {
+    if (n_seqs < 1) return -1;
+    int lo = 0, hi = n_seqs + 1;                    // the answer is the last index in [lo, hi) whose offset is at most r
+    bool none = false;
+    while (hi - lo > 1 || lo == 0) {
+        const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+        const int below = __popcll(__ballot(at < hi && row_offsets[at] <= r));
+        if (below == 0) { none = true; break; }
+        lo += (below - 1) * step;
+        hi = min(lo + step, hi);
+        if (step == 1) break;
+    }
+    return none || lo >= n_seqs ? -1 : lo;
+}
+
 // ATTS_OK, or the error of a cache that no kernel can read; *view is filled in.
 int32_t check_paged(const char* fn, const atts_paged_cache* cache, PagedView* view);
 
