@@ -53,44 +53,186 @@ struct AppendArgs {
     const float2* table;
     int64_t qkv_stride;
     int32_t R, nq, n_positions, half, interleaved;
+    int32_t heads_each, turned_chunks, values_each;      // set by launch_append: heads of a workgroup, chunks of query and key heads
 };
 
-template <typename T>
+// Rows r0 .. r0 + n - 1 (n <= 64) of a workgroup: each one's token and page in its sequence's cache, page -1 if it has none.  By one wavefront: the
+// sequences of the first and the last row by a search of the whole wavefront, of those between by counting offsets.
+struct Places {
+    int32_t token[64], page[64];
+    __device__ void find(const PagedView& p, const AppendArgs& a, int r0, int n, int lane) {
+        const int s0 = sequence_of_wave(a.row_offsets, p.n_seqs, r0, lane), s1 = sequence_of_wave(a.row_offsets, p.n_seqs, r0 + n - 1, lane);
+        int seq = s0;
+        if (s0 < 0 || s1 < 0 || s1 - s0 > 64) seq = lane < n ? sequence_of(a.row_offsets, p.n_seqs, r0 + lane) : -1;
+        else if (s1 > s0) {
+            const int next = s0 + 1 + lane <= s1 ? a.row_offsets[s0 + 1 + lane] : 0x7fffffff;
+            for (int i = 0; i < n; ++i) {
+                const int owner = s0 + __popcll(__ballot(next <= r0 + i));
+                if (lane == i) seq = owner;
+            }
+        }
+        int at = -1, where = 0;
+        if (lane < n && seq >= 0) {
+            const int64_t t = (int64_t)a.cached[seq] + (r0 + lane - a.row_offsets[seq]);
+            if (t >= 0 && t < p.slots()) {
+                where = (int)t;
+                at = p.page_of(seq, where);
+                if ((uint32_t)at >= (uint32_t)p.n_pages) at = -1;
+            }
+        }
+        token[lane] = where;
+        page[lane] = at;
+    }
+};
+
+// A workgroup: 64 rows, and a few query and key heads or (the last ones of a grid's y) a few value heads.
+//   * Queries and keys: a thread keeps the cosines and sines of its piece of a row for all its heads.  PIECE elements are 16 bytes; a piece of the first
+//     half turns with its partner half a rotation on (or within itself, interleaved).
+//   * Values go through LDS: a thread gathers the tokens of one head element that lie side by side in the page and writes 16 bytes of them;
+//     tokens that do not fill such a place are written by themselves.
+// PIECE 1: any alignment and rotation.
+template <typename T, int PIECE>
 __global__ __launch_bounds__(256) void rotary_append_kernel(const T* __restrict__ qkv, T* __restrict__ q_out, T* __restrict__ k_pages,
                                                             T* __restrict__ v_pages, PagedView p, AppendArgs a) {
-    const int r = blockIdx.x;
-    const int seq = sequence_of(a.row_offsets, p.n_seqs, r);
-    int page = -1, token = 0;
-    if (seq >= 0) {
-        const int64_t at = (int64_t)a.cached[seq] + (r - a.row_offsets[seq]);
-        if (at >= 0 && at < p.slots()) {
-            token = (int)at;
-            page = p.page_of(seq, token);
-            if (page >= p.n_pages) page = -1;
+    typedef T Vec __attribute__((ext_vector_type(PIECE)));
+    constexpr int kGroup = 16 / sizeof(T);               // tokens of a 16-byte store
+    __shared__ Places places;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, r0 = blockIdx.x * 64, n = min(64, a.R - r0), hd = p.hd, turned = a.nq + p.n_kv;
+    const int first = (int)blockIdx.y * a.heads_each;
+    const bool values = (int)blockIdx.y >= a.turned_chunks;
+    if (!values) {
+        const int last = min(first + a.heads_each, turned), rot = 2 * a.half;
+        if (last > a.nq) {                                   // the workgroup has keys
+            if (tid < 64) places.find(p, a, r0, n, tid);
+            __syncthreads();
+        }
+        // pieces of a head: those that turn with a partner (one for two), then those that stay or turn within themselves
+        const int pairs = a.interleaved ? 0 : a.half / PIECE, pieces = pairs + (hd - 2 * pairs * PIECE) / PIECE;
+        for (int item = tid; item < n * pieces; item += 256) {
+            const int i = item / pieces, piece = item - i * pieces, r = r0 + i;
+            const bool pair = piece < pairs;
+            const int e = pair ? piece * PIECE : rot * (pairs > 0) + (piece - pairs) * PIECE;
+            const float2* cs = a.table + (int64_t)min(max(a.positions[r], 0), a.n_positions - 1) * a.half;
+            const bool inside = a.interleaved && PIECE > 1 && e < rot;
+            float c[PIECE], s[PIECE];
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) {
+                float2 t = make_float2(1.f, 0.f);
+                if (pair) t = cs[e + j];
+                else if (inside && e + j < rot) t = cs[(e + j) >> 1];
+                c[j] = t.x;
+                s[j] = t.y;
+            }
+            const T* src = qkv + (int64_t)r * a.qkv_stride;
+#pragma unroll 4
+            for (int head = first; head < last; ++head) {
+                T* dst;
+                if (head < a.nq) dst = q_out + ((int64_t)r * a.nq + head) * hd;
+                else if (places.page[i] >= 0) dst = k_pages + p.key_at(places.page[i], head - a.nq, places.token[i]);
+                else continue;
+                const T* from = src + (int64_t)head * hd;
+                if constexpr (PIECE == 1) {                  // one element, its partner read beside it
+                    for (int half = 0; half <= (int)pair; ++half) {
+                        const int x = e + half * a.half;
+                        float y = to_f32(from[x]);
+                        if (pair) y = half ? y * c[0] + to_f32(from[x - a.half]) * s[0] : y * c[0] - to_f32(from[x + a.half]) * s[0];
+                        else if (a.interleaved && x < rot) {
+                            const float2 t = cs[x >> 1];
+                            y = x & 1 ? y * t.x + to_f32(from[x - 1]) * t.y : y * t.x - to_f32(from[x + 1]) * t.y;
+                        }
+                        dst[x] = from_f32<T>(y);
+                    }
+                } else {
+                    const Vec x = *reinterpret_cast<const Vec*>(from + e);
+                    Vec y;
+                    if (pair) {
+                        const Vec z = *reinterpret_cast<const Vec*>(from + e + a.half);
+                        Vec w;
+#pragma unroll
+                        for (int j = 0; j < PIECE; ++j) {
+                            y[j] = from_f32<T>(to_f32((T)x[j]) * c[j] - to_f32((T)z[j]) * s[j]);
+                            w[j] = from_f32<T>(to_f32((T)z[j]) * c[j] + to_f32((T)x[j]) * s[j]);
+                        }
+                        *reinterpret_cast<Vec*>(dst + e + a.half) = w;
+                    } else if (inside) {
+#pragma unroll
+                        for (int j = 0; j < PIECE; j += 2) {
+                            const float u = to_f32((T)x[j]), v = to_f32((T)x[j + 1]);
+                            y[j] = from_f32<T>(u * c[j] - v * s[j]);
+                            y[j + 1] = from_f32<T>(v * c[j] + u * s[j]);
+                        }
+                    } else y = x;
+                    *reinterpret_cast<Vec*>(dst + e) = y;
+                }
+            }
+        }
+        return;
+    }
+    if (tid < 64) places.find(p, a, r0, n, tid);
+    __syncthreads();
+    T* const tile = reinterpret_cast<T*>(smem);              // [64][hd + 1]: an odd pitch, so that rows eight apart fall into different banks
+    const int pitch = hd + 1, h0 = ((int)blockIdx.y - a.turned_chunks) * a.values_each, h1 = min(h0 + a.values_each, p.n_kv);
+    // groups of rows begin where the first row's page has a 16-byte place
+    const int lead = (kGroup - places.token[0] % kGroup) % kGroup, groups = (n - lead + kGroup - 1) / kGroup + (lead > 0);
+    for (int h = h0; h < h1; ++h) {
+        if (h > h0) __syncthreads();
+        for (int item = tid; item < n * hd / PIECE; item += 256) {
+            const int i = item / (hd / PIECE), e = (item - i * (hd / PIECE)) * PIECE;
+            const T* from = qkv + (int64_t)(r0 + i) * a.qkv_stride + (int64_t)(turned + h) * hd + e;
+            if constexpr (PIECE == 1) tile[i * pitch + e] = *from;
+            else {
+                const Vec x = *reinterpret_cast<const Vec*>(from);
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) tile[i * pitch + e + j] = x[j];
+            }
+        }
+        __syncthreads();
+        for (int item = tid; item < groups * hd; item += 256) {
+            const int d = item / groups, g = item - d * groups;
+            const int i0 = lead > 0 ? (g ? lead + (g - 1) * kGroup : 0) : g * kGroup, i1 = min(lead > 0 && g == 0 ? lead : i0 + kGroup, n);
+            const int page = places.page[i0], token = places.token[i0];
+            // a whole place: kGroup tokens of one page, one behind the other (page sizes are multiples of it)
+            bool whole = i1 - i0 == kGroup && page >= 0 && token % kGroup == 0;
+            if (whole) whole = places.page[i0 + kGroup - 1] == page && places.token[i0 + kGroup - 1] == token + kGroup - 1;
+            if (whole)
+                for (int i = i0 + 1; i < i1 - 1; ++i) whole &= places.page[i] == page && places.token[i] == token + i - i0;
+            if (whole) {
+                typedef T Group __attribute__((ext_vector_type(kGroup)));
+                Group y;
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j) y[j] = tile[(i0 + j) * pitch + d];
+                *reinterpret_cast<Group*>(v_pages + p.value_at(page, h, token) + ((int64_t)d << p.page_log)) = y;
+            } else {
+                for (int i = i0; i < i1; ++i)
+                    if (places.page[i] >= 0) v_pages[p.value_at(places.page[i], h, places.token[i]) + ((int64_t)d << p.page_log)] = tile[i * pitch + d];
+            }
         }
     }
-    const float2* cs = a.table + (int64_t)min(max(a.positions[r], 0), a.n_positions - 1) * a.half;
-    const T* src = qkv + (int64_t)r * a.qkv_stride;
-    const int hd = p.hd, heads = a.nq + 2 * p.n_kv, rot = 2 * a.half;
-    for (int e = threadIdx.x; e < heads * hd; e += 256) {
-        const int head = e / hd, i = e - head * hd;
-        float y = to_f32(src[e]);
-        if (head < a.nq + p.n_kv && i < rot) {
-            int pair, other;
-            bool second;
-            if (a.interleaved) { pair = i >> 1; second = i & 1; other = i ^ 1; }
-            else { second = i >= a.half; pair = second ? i - a.half : i; other = second ? i - a.half : i + a.half; }
-            const float2 t = cs[pair];
-            const float o = to_f32(src[head * hd + other]);
-            y = second ? y * t.x + o * t.y : y * t.x - o * t.y;
-        }
-        if (head < a.nq) q_out[(int64_t)r * a.nq * hd + e] = from_f32<T>(y);
-        else if (page >= 0) {
-            const int h = head - a.nq;
-            if (h < p.n_kv) k_pages[p.key_at(page, h, token) + i] = from_f32<T>(y);
-            else v_pages[p.value_at(page, h - p.n_kv, token) + ((int64_t)i << p.page_log)] = from_f32<T>(y);
-        }
-    }
+}
+
+template <typename T>
+int32_t launch_append(const atts_paged_cache& c, const void* qkv, void* q_out, const PagedView& p, AppendArgs a, hipStream_t stream) {
+    constexpr int kPiece = 16 / sizeof(T);
+    const int64_t blocks = ceil_div(a.R, 64), turned = (int64_t)a.nq + p.n_kv;
+    // about four workgroups a compute unit: with fewer rows a head each, with many the table's rows are read once for several heads
+    a.heads_each = (int32_t)(turned * blocks / 1024 < 1 ? 1 : turned * blocks / 1024 > 16 ? 16 : turned * blocks / 1024);
+    a.turned_chunks = (int32_t)ceil_div(turned, a.heads_each);
+    a.values_each = 1;
+    const bool pieces = !(((uintptr_t)qkv | (uintptr_t)q_out | (uint64_t)a.qkv_stride * sizeof(T)) & 15) && a.half % (a.interleaved ? 1 : kPiece) == 0 &&
+                        (!a.interleaved || 2 * a.half % kPiece == 0);
+    const dim3 grid((unsigned)blocks, (unsigned)(a.turned_chunks + ceil_div(p.n_kv, a.values_each)));
+    const size_t lds = (size_t)64 * (p.hd + 1) * sizeof(T);
+    const auto run = [&](auto kernel, int32_t allowed) {
+        if (allowed != ATTS_OK) return allowed;
+        hipLaunchKernelGGL(kernel, grid, dim3(256), lds, stream, static_cast<const T*>(qkv), static_cast<T*>(q_out), static_cast<T*>(c.k_pages),
+                           static_cast<T*>(c.v_pages), p, a);
+        ATTS_LAUNCH_CHECK("rotary_append_kernel");
+        return (int32_t)ATTS_OK;
+    };
+    constexpr size_t most = 64 * 257 * sizeof(T);
+    return pieces ? run(rotary_append_kernel<T, kPiece>, allow_dynamic_lds<rotary_append_kernel<T, kPiece>>(most))
+                  : run(rotary_append_kernel<T, 1>, allow_dynamic_lds<rotary_append_kernel<T, 1>>(most));
 }
 
 }  // namespace
@@ -142,16 +284,9 @@ int32_t atts_rotary_append(const atts_paged_cache* cache, const void* qkv, int64
     if (rot_dim > 0 && (!table || ((uintptr_t)table & 7) || n_positions < 1)) return fail(ATTS_ERR_INVALID_ARG, "%s: table NULL, empty or not 8-byte aligned", fn);
     if (qkv_stride < (int64_t)(n_q_heads + 2 * p.n_kv) * p.hd) return fail(ATTS_ERR_INVALID_ARG, "%s: rows of qkv overlap", fn);
     const AppendArgs a{positions, cached, row_offsets, reinterpret_cast<const float2*>(table), qkv_stride, R, n_q_heads,
-                       n_positions < 1 ? 1 : n_positions, rot_dim / 2, layout == ATTS_ROTARY_INTERLEAVED};
+                       n_positions < 1 ? 1 : n_positions, rot_dim / 2, layout == ATTS_ROTARY_INTERLEAVED, 0, 0, 0};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (cache->dtype == ATTS_DTYPE_F32)
-        hipLaunchKernelGGL(rotary_append_kernel<float>, dim3((unsigned)R), dim3(256), 0, stream, static_cast<const float*>(qkv),
-                           static_cast<float*>(q_out), static_cast<float*>(cache->k_pages), static_cast<float*>(cache->v_pages), p, a);
-    else
-        hipLaunchKernelGGL(rotary_append_kernel<bf16>, dim3((unsigned)R), dim3(256), 0, stream, static_cast<const bf16*>(qkv),
-                           static_cast<bf16*>(q_out), static_cast<bf16*>(cache->k_pages), static_cast<bf16*>(cache->v_pages), p, a);
-    ATTS_LAUNCH_CHECK("rotary_append_kernel");
-    return ATTS_OK;
+    return cache->dtype == ATTS_DTYPE_F32 ? launch_append<float>(*cache, qkv, q_out, p, a, stream) : launch_append<bf16>(*cache, qkv, q_out, p, a, stream);
 }
 
 }  // extern "C"
