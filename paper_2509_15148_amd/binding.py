@@ -117,7 +117,7 @@ except ImportError:
         @staticmethod
         def calibrate_online(*args):
             return _marshal.OTHER
-        classify_ordinal = classify_conditional = calibrate_online
+        classify_ordinal = classify_conditional = gemm_nt_quant = rotary_append = attention_tree = logits_adjust = calibrate_online
 
 
 def _check(rc: int) -> None:
@@ -519,6 +519,9 @@ def atts_gemm_nt_quant(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
                        epilogue: int = EPILOGUE_STORE, residual: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """out = x W^T with W in 4-bit codes [rows, K / 2], scales and zeros [rows, K / group] (see atts.h for the epilogues).  Without a workspace, a
     call that needs one takes it from torch's allocator for its own duration on the current stream."""
+    rc = _marshal.gemm_nt_quant(x, codes, scales, zeros, out, epilogue, residual, workspace)
+    if rc != _marshal.OTHER:
+        return _check(rc)
     if x.dim() != 2 or codes.dim() != 2 or scales.dim() != 2 or out.dim() != 2:
         raise AttsError(ERR_INVALID_ARG, "x, codes, scales and out must be matrices")
     (M, K), wide, groups = x.shape, codes.shape[0], scales.shape[1]
@@ -527,10 +530,14 @@ def atts_gemm_nt_quant(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
             (epilogue == EPILOGUE_SWIGLU and wide % 2) or (zeros is not None and zeros.shape != scales.shape) or \
             (epilogue == EPILOGUE_RESIDUAL and (residual is None or residual.shape != out.shape)):
         raise AttsError(ERR_INVALID_ARG, "shape mismatch")
-    xp, ld = _rows(x, x.dtype, "x")
     if workspace is None and M > 16:                    # up to 16 rows nothing is cut
         need = atts_gemm_nt_quant_workspace_bytes(x.dtype, M, N, K, epilogue)
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+            rc = _marshal.gemm_nt_quant(x, codes, scales, zeros, out, epilogue, residual, workspace)
+            if rc != _marshal.OTHER:
+                return _check(rc)
+    xp, ld = _rows(x, x.dtype, "x")
     _check(_lib.atts_gemm_nt_quant(_dtype_code(x.dtype), xp, ld, _ptr(codes, torch.uint8, "codes"), _ptr(scales, x.dtype, "scales"),
                                    _ptr(zeros, torch.uint8, "zeros"), K // groups,
                                    _ptr(residual, torch.float32, "residual") if epilogue == EPILOGUE_RESIDUAL else None,
@@ -583,6 +590,9 @@ class PagedCache:
 
 def atts_rotary_append(cache: PagedCache, qkv: torch.Tensor, positions: torch.Tensor, cached: torch.Tensor, row_offsets: torch.Tensor,
                        table: torch.Tensor, layout: int, q_out: torch.Tensor) -> None:
+    rc = _marshal.rotary_append(cache.handle, qkv, positions, cached, row_offsets, table, layout, q_out)
+    if rc != _marshal.OTHER:
+        return _check(rc)
     if qkv.dim() != 2 or table.dim() != 3 or table.shape[2] != 2 or q_out.dim() != 2:
         raise AttsError(ERR_INVALID_ARG, "qkv and q_out must be matrices, table [positions, rot_dim / 2, 2]")
     R, hd = qkv.shape[0], cache.head_dim
@@ -608,6 +618,9 @@ def atts_attention_tree(cache: PagedCache, q: torch.Tensor, parents: torch.Tenso
                         max_cached: int, out: torch.Tensor, workspace: Optional[torch.Tensor], scale: Optional[float] = None,
                         softcap: float = 0.0, window: int = 0) -> None:
     """scale: 1 / sqrt(head_dim) unless given"""
+    rc = _marshal.attention_tree(cache.handle, q, parents, cached, row_offsets, max_rows, max_cached, out, workspace, scale, softcap, window)
+    if rc != _marshal.OTHER:
+        return _check(rc)
     if q.dim() != 2 or q.shape[1] % cache.head_dim or out.shape != q.shape:
         raise AttsError(ERR_INVALID_ARG, "q and out must both be [R, n_q_heads head_dim]")
     R = q.shape[0]
@@ -633,6 +646,10 @@ def atts_logits_adjust(logits: torch.Tensor, row_offsets: torch.Tensor, params: 
                        bias_offsets: Optional[torch.Tensor], mask: Optional[torch.Tensor], out: torch.Tensor, top_ids: Optional[torch.Tensor],
                        lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor], max_rows: Optional[int] = None) -> None:
     """mask: int32 words of 32 bits, [R, ceil(V / 32)].  max_rows: the rows of the longest sequence (unless given, as many as there can be)"""
+    rc = _marshal.logits_adjust(logits, row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_values, bias_offsets,
+                                mask, out, top_ids, lse, workspace, max_rows)
+    if rc != _marshal.OTHER:
+        return _check(rc)
     if logits.dim() != 2 or out.shape != logits.shape:
         raise AttsError(ERR_INVALID_ARG, "logits and out must both be [R, V]")
     (R, V), S = logits.shape, row_offsets.numel() - 1

@@ -1,5 +1,5 @@
-// Argument marshalling of the short calls (module _marshal): append, verdict and conditional verdict take their tensors as they are,
-// check them and call the library.  A launch takes about 4 us of host time; the checks and conversions of up to eight tensors took
+// Argument marshalling of the short calls (module _marshal): append, verdict and conditional verdict, and the operators of a step over drafted
+// trees, take their tensors as they are, check them and call the library.  A launch takes about 4 us of host time; the checks and conversions of up to eight tensors took
 // 2 to 3 more in Python, on calls whose kernels take 3 to 6.
 //
 // Every function returns the library's status, or kOther when an argument is not the plain one it is made for (another type, dtype or
@@ -10,6 +10,8 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+
+#include <cmath>
 
 #include "atts.h"
 
@@ -153,8 +155,187 @@ PyObject* classify_conditional(PyObject*, PyObject* const* a, Py_ssize_t n) {   
     });
 }
 
+// ---- operators of a step over drafted trees -------------------------------------------------------------------------
+
+struct Matrix {
+    void* data = nullptr;
+    int64_t rows = 0, cols = 0, stride = 0;
+};
+
+// a device matrix of the type with contiguous rows
+bool take_rows(PyObject* o, at::ScalarType type, Matrix& out) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 2) return false;
+    const auto size = t.sizes(), stride = t.strides();
+    if (size[0] < 1 || size[1] < 1 || (size[1] > 1 && stride[1] != 1)) return false;
+    out = {t.data_ptr(), size[0], size[1], size[0] > 1 ? stride[0] : size[1]};
+    return true;
+}
+
+// a contiguous one
+bool take_matrix(PyObject* o, at::ScalarType type, Matrix& out) { return take_rows(o, type, out) && out.stride == out.cols; }
+
+// bf16 or fp32, as the first matrix of a call is
+bool take_type(PyObject* o, at::ScalarType& type, int32_t& dtype) {
+    if (!THPVariable_CheckExact(o)) return false;
+    type = THPVariable_Unpack(o).scalar_type();
+    dtype = type == at::kFloat ? ATTS_DTYPE_F32 : ATTS_DTYPE_BF16;
+    return type == at::kFloat || type == at::kBFloat16;
+}
+
+bool take_int(PyObject* o, int32_t& out) {
+    if (!PyLong_CheckExact(o)) return false;
+    int over = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+    if (over || v < INT32_MIN || v > INT32_MAX) return false;
+    out = (int32_t)v;
+    return true;
+}
+
+// an array of exactly n elements, not empty; optional: or None
+bool take_n(PyObject* o, at::ScalarType type, bool optional, int64_t n, Array& out) {
+    return take(o, type, optional, out) && (o == Py_None || (out.n == n && n > 0));
+}
+
+PyObject* gemm_nt_quant(PyObject*, PyObject* const* a, Py_ssize_t n) {          // x, codes, scales, zeros, out, epilogue, residual, workspace
+    return guarded([&]() -> long {
+        void* stream;
+        at::ScalarType type;
+        int32_t dtype, epilogue;
+        Matrix x, codes, scales, out;
+        Array zeros, residual, workspace;
+        if (n != 8 || !take_type(a[0], type, dtype) || !take_rows(a[0], type, x) || !take_matrix(a[1], at::kByte, codes) || !take_matrix(a[2], type, scales) ||
+            !take(a[3], at::kByte, true, zeros) || !take_int(a[5], epilogue) || epilogue < ATTS_EPILOGUE_STORE || epilogue > ATTS_EPILOGUE_SWIGLU ||
+            !take(a[7], at::kByte, true, workspace))
+            return kOther;
+        const bool swiglu = epilogue == ATTS_EPILOGUE_SWIGLU, adds = epilogue == ATTS_EPILOGUE_RESIDUAL;
+        if (!take_matrix(a[4], adds || epilogue == ATTS_EPILOGUE_STORE_F32 ? at::kFloat : type, out) || (adds && !take(a[6], at::kFloat, false, residual)))
+            return kOther;
+        if (codes.cols * 2 != x.cols || scales.rows != codes.rows || x.cols % scales.cols || (swiglu && codes.rows % 2) || out.rows != x.rows ||
+            out.cols != (swiglu ? codes.rows / 2 : codes.rows) || (a[3] != Py_None && zeros.n != scales.rows * scales.cols) ||
+            (adds && residual.n != out.rows * out.cols) || x.rows > INT32_MAX || x.cols > INT32_MAX || codes.rows > INT32_MAX)
+            return kOther;
+        const int32_t M = (int32_t)x.rows, N = (int32_t)out.cols, K = (int32_t)x.cols, group = (int32_t)(x.cols / scales.cols);
+        size_t need = 0;
+        if (a[7] == Py_None && (atts_gemm_nt_quant_workspace_bytes(dtype, M, N, K, epilogue, &need) != ATTS_OK || need > 0)) return kOther;
+        if (!take_stream(stream)) return kOther;
+        int32_t rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = atts_gemm_nt_quant(dtype, x.data, x.stride, static_cast<const uint8_t*>(codes.data), scales.data, static_cast<const uint8_t*>(zeros.data), group,
+                                static_cast<const float*>(residual.data), out.data, M, N, K, epilogue, workspace.data, (size_t)workspace.n, stream);
+        Py_END_ALLOW_THREADS
+        return rc;
+    });
+}
+
+// the description behind a PagedCache's handle, with its arrays' type
+bool take_cache(PyObject* o, const atts_paged_cache*& cache, at::ScalarType& type) {
+    void* handle;
+    if (!take_handle(o, handle)) return false;
+    cache = static_cast<const atts_paged_cache*>(handle);
+    type = cache->dtype == ATTS_DTYPE_F32 ? at::kFloat : at::kBFloat16;
+    return true;
+}
+
+PyObject* rotary_append(PyObject*, PyObject* const* a, Py_ssize_t n) {          // handle, qkv, positions, cached, row_offsets, table, layout, q_out
+    return guarded([&]() -> long {
+        void* stream;
+        const atts_paged_cache* c;
+        at::ScalarType type;
+        int32_t layout;
+        Matrix qkv, q_out;
+        Array positions, cached, offsets, table;
+        if (n != 8 || !take_cache(a[0], c, type) || !take_rows(a[1], type, qkv) || !take_int(a[6], layout) || !take_matrix(a[7], type, q_out) ||
+            !take_n(a[2], at::kInt, false, qkv.rows, positions) || !take_n(a[3], at::kInt, false, c->n_seqs, cached) ||
+            !take_n(a[4], at::kInt, false, (int64_t)c->n_seqs + 1, offsets) || !take(a[5], at::kFloat, false, table))
+            return kOther;
+        const at::Tensor& t = THPVariable_Unpack(a[5]);
+        const int64_t hd = c->head_dim, heads = qkv.cols / hd - 2 * (int64_t)c->n_kv_heads;
+        if (t.dim() != 3 || t.size(2) != 2 || t.size(0) < 1 || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX / 2 || heads < 1 || heads > INT32_MAX ||
+            qkv.cols != (heads + 2 * c->n_kv_heads) * hd || q_out.rows != qkv.rows || q_out.cols != heads * hd || qkv.rows > INT32_MAX || !take_stream(stream))
+            return kOther;
+        int32_t rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = atts_rotary_append(c, qkv.data, qkv.stride, static_cast<const int32_t*>(positions.data), static_cast<const int32_t*>(cached.data),
+                                static_cast<const int32_t*>(offsets.data), (int32_t)qkv.rows, (int32_t)heads, static_cast<const float*>(table.data),
+                                (int32_t)t.size(0), (int32_t)(2 * t.size(1)), layout, q_out.data, stream);
+        Py_END_ALLOW_THREADS
+        return rc;
+    });
+}
+
+// handle, q, parents, cached, row_offsets, max_rows, max_cached, out, workspace, scale (or None), softcap, window
+PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> long {
+        void* stream;
+        const atts_paged_cache* c;
+        at::ScalarType type;
+        int32_t max_rows, max_cached, window;
+        Matrix q, out;
+        Array parents, cached, offsets, workspace;
+        if (n != 12 || !take_cache(a[0], c, type) || !take_matrix(a[1], type, q) || !take_matrix(a[7], type, out) ||
+            !take_n(a[2], at::kInt, false, q.rows, parents) || !take_n(a[3], at::kInt, false, c->n_seqs, cached) ||
+            !take_n(a[4], at::kInt, false, (int64_t)c->n_seqs + 1, offsets) || !take_int(a[5], max_rows) || !take_int(a[6], max_cached) ||
+            !take(a[8], at::kByte, true, workspace) || (a[9] != Py_None && !PyFloat_CheckExact(a[9])) || !PyFloat_CheckExact(a[10]) || !take_int(a[11], window))
+            return kOther;
+        const int64_t hd = c->head_dim;
+        if (q.cols % hd || out.rows != q.rows || out.cols != q.cols || q.rows > INT32_MAX || q.cols / hd > INT32_MAX || !take_stream(stream)) return kOther;
+        const double scale = a[9] != Py_None ? PyFloat_AS_DOUBLE(a[9]) : std::pow((double)hd, -0.5);
+        int32_t rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = atts_attention_tree(c, q.data, static_cast<const int32_t*>(parents.data), static_cast<const int32_t*>(cached.data),
+                                 static_cast<const int32_t*>(offsets.data), (int32_t)q.rows, (int32_t)(q.cols / hd), max_rows, max_cached, (float)scale,
+                                 (float)PyFloat_AS_DOUBLE(a[10]), window, out.data, workspace.data, (size_t)workspace.n, stream);
+        Py_END_ALLOW_THREADS
+        return rc;
+    });
+}
+
+// logits, row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_values, bias_offsets, mask, out, top_ids, lse,
+// workspace, max_rows (or None)
+PyObject* logits_adjust(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> long {
+        void* stream;
+        at::ScalarType type;
+        int32_t dtype, max_rows;
+        Matrix logits, out;
+        Array offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_values, bias_offsets, mask, top_ids, lse, workspace;
+        if (n != 17 || !take_type(a[0], type, dtype) || !take_rows(a[0], type, logits) || !take_rows(a[12], type, out) || !take(a[1], at::kInt, false, offsets) ||
+            offsets.n < 2)
+            return kOther;
+        const int64_t R = logits.rows, V = logits.cols, S = offsets.n - 1, words = (V + 31) / 32;
+        if (!take_n(a[2], at::kFloat, true, 4 * S, params) || !take(a[3], at::kInt, true, history) || (a[3] != Py_None && history.n == 0) ||
+            !take_n(a[4], at::kInt, true, S + 1, history_offsets) || !take_n(a[5], at::kInt, true, S, prompt_lens) ||
+            !take_n(a[6], at::kInt, true, R, tree_ids) || !take_n(a[7], at::kInt, true, R, parents) || !take(a[8], at::kInt, true, bias_ids) ||
+            (a[8] != Py_None && bias_ids.n == 0) || (a[8] == Py_None) != (a[9] == Py_None) || !take_n(a[9], at::kFloat, true, bias_ids.n, bias_values) ||
+            !take_n(a[10], at::kInt, true, S + 1, bias_offsets) || !take_n(a[11], at::kInt, true, R * words, mask) ||
+            !take_n(a[13], at::kInt, true, R, top_ids) || !take_n(a[14], at::kFloat, true, R, lse) || !take(a[15], at::kByte, true, workspace))
+            return kOther;
+        if (a[11] != Py_None) {
+            const at::Tensor& m = THPVariable_Unpack(a[11]);
+            if (m.dim() != 2 || m.size(0) != R) return kOther;
+        }
+        if (a[16] == Py_None) max_rows = (int32_t)(R < ATTS_MAX_TREE ? R : ATTS_MAX_TREE);
+        else if (!take_int(a[16], max_rows)) return kOther;
+        if (out.rows != R || out.cols != V || R > INT32_MAX || V > INT32_MAX || S > INT32_MAX || history.n > INT32_MAX || bias_ids.n > INT32_MAX || !take_stream(stream))
+            return kOther;
+        const auto i32 = [](const Array& x) { return static_cast<const int32_t*>(x.data); };
+        int32_t rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = atts_logits_adjust(dtype, logits.data, logits.stride, i32(offsets), (int32_t)S, max_rows, static_cast<const float*>(params.data), i32(history),
+                                i32(history_offsets), i32(prompt_lens), (int32_t)history.n, i32(tree_ids), i32(parents), i32(bias_ids),
+                                static_cast<const float*>(bias_values.data), i32(bias_offsets), (int32_t)bias_ids.n, static_cast<const uint32_t*>(mask.data),
+                                (int32_t)R, (int32_t)V, out.data, out.stride, static_cast<int32_t*>(top_ids.data), static_cast<float*>(lse.data),
+                                workspace.data, (size_t)workspace.n, stream);
+        Py_END_ALLOW_THREADS
+        return rc;
+    });
+}
+
 #define ATTS_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ATTS_METHOD(setup), ATTS_METHOD(calibrate_online), ATTS_METHOD(classify_ordinal), ATTS_METHOD(classify_conditional),
+                         ATTS_METHOD(gemm_nt_quant), ATTS_METHOD(rotary_append), ATTS_METHOD(attention_tree), ATTS_METHOD(logits_adjust),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
