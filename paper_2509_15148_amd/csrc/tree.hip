@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace atts {
 namespace {
@@ -38,7 +39,8 @@ struct TreeArgs {
     float* part_o;               // [R n_q, max_splits, hd] sums of a split relative to its reference, [R n_q, max_splits] (reference, sum)
     float2* part_ml;
     int32_t R, nq, max_rows, max_cached, window, max_splits, tiles_per_split, row_tiles, n_groups;
-    float scale, softcap;        // scale: log2(e) scale, or without a cap's factor
+    int32_t negate;              // the scale is negative: the queries' signs are turned, which is exact
+    float scale, softcap;        // scale: |scale| log2(e), or with a cap 2 log2(e) |scale| / softcap; softcap: log2(e) softcap
 };
 
 // What a sequence is to its workgroups; every value is the same for all lanes.
@@ -83,7 +85,7 @@ __device__ __forceinline__ bool any_not_finite(f32x4 v) { return not_finite(v[0]
 
 // HD: head_dim, or the next size up when EXACT is false; QT: tiles of 16 query rows.
 template <typename T, int HD, int QT, bool EXACT>
-__global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void tree_attention_kernel(
+__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
         const T* __restrict__ q, const T* __restrict__ k_pages, const T* __restrict__ v_pages, T* __restrict__ out, PagedView p, TreeArgs a) {
     using X = Shape<T>;
     using Vec = typename X::Vec;
@@ -106,19 +108,28 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, c = lane >> 4;
     const bool tree_here = s.lo + tile1 * X::kKeys > s.L || a.window != 0;
 
-    Vec qf[QT][kSteps];
+    // Queries: in registers, or, 64 rows, in LDS, fragment by fragment as the lanes take them: with them the accumulators would not fit the
+    // registers that the vector unit reaches, and move to and fro.
+    constexpr bool kQueriesInLds = QT > 2;
+    __shared__ Vec lds_q[kQueriesInLds ? QT * kSteps * 64 : 1];
+    Vec qf[kQueriesInLds ? 1 : QT][kSteps];
     int own[QT];                                          // the row of the tree a query row belongs to
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int m = row_tile * kRows + t * 16 + r;
         own[t] = min(m / group, s.n - 1);
+        if (kQueriesInLds && t != wave) continue;           // wavefront t writes the fragments of tile t
         const T* src = q + ((int64_t)(s.first + own[t]) * a.nq + kv * group + m % group) * hd;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int d = i * X::kStep + c * X::kElems;
-            qf[t][i] = m < n_rows && (EXACT || d < hd) ? *reinterpret_cast<const Vec*>(src + d) : Vec{};
+            Vec one = m < n_rows && (EXACT || d < hd) ? *reinterpret_cast<const Vec*>(src + d) : Vec{};
+            if (a.negate) one = -one;
+            if constexpr (kQueriesInLds) lds_q[(t * kSteps + i) * 64 + lane] = one;
+            else qf[t][i] = one;
         }
     }
+    if (kQueriesInLds) __syncthreads();
     if (tree_here) {
         int up = -1;
         if (tid < s.n) {
@@ -155,9 +166,6 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
         }
         __syncthreads();
     }
-    // tiles [open0, open1) are seen whole by every row: behind the last row's window, before the tree
-    const int open0 = a.window ? s.L + s.n - a.window : 0, open1 = s.L;
-
     // Key rows of the first product: lane row r of sub-tile u is key 8 (r / 4) + 4 u + r % 4 (bf16), key r (fp32).
     const int k_slot = X::kSub == 2 ? 8 * (r >> 2) + (r & 3) : r, v_slot = kE * c;
     auto page_at = [&](int token) {
@@ -196,54 +204,32 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
         for (int i = 0; i < kDims; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int my0 = tile0 + wave;
-    int key0 = s.lo + my0 * X::kKeys;
-    int pk = 0, pv = 0, pk_next = 0, pv_next = 0;         // pages of this and the next tile
-    if (my0 < tile1) {
-        pk = page_at(key0 + k_slot);
-        pv = page_at(key0 + v_slot);
-        pk_next = page_at(key0 + kTreeWaves * X::kKeys + k_slot);
-        pv_next = page_at(key0 + kTreeWaves * X::kKeys + v_slot);
-        load_keys(pk, key0);
-        load_values(pv, key0);
-    }
-    for (int tile = my0; tile < tile1; tile += kTreeWaves) {
-        const int next0 = key0 + kTreeWaves * X::kKeys;
-        const bool more = tile + kTreeWaves < tile1;
-        f32x4 z[QT][X::kSub];
+    // One tile of keys, in kf and vf; `refill` requests the next keys once these are used.  MASKED: some row may not see some key.
+    auto attend = [&](auto masked, int key0, int page, auto&& refill) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked)::value;
+        float e[QT][kE];
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int u = 0; u < X::kSub; ++u) {
-                z[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+                f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) z[t][u] = mma(kf[u][i], qf[t][i], z[t][u]);
+                for (int i = 0; i < kSteps; ++i) z = mma(kf[u][i], kQueriesInLds ? lds_q[(t * kSteps + i) * 64 + lane] : qf[kQueriesInLds ? 0 : t][i], z);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) e[t][u * 4 + x] = z[x];
             }
-        const int pv_now = pv;
-        if (more) {
-            load_keys(pk_next, next0);
-            pk_next = page_at(next0 + kTreeWaves * X::kKeys + k_slot);
-        }
-
-        float e[QT][kE];
+        refill();
+        float by = a.scale;                                                 // what turns e into units of log2
         if (a.softcap > 0.f) {
 #pragma unroll
             for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int j = 0; j < kE; ++j) {
-                    // cap tanh(x) with tanh x = 1 - 2 / (1 + exp 2x), in units of log2
-                    const float g = __builtin_amdgcn_exp2f(z[t][j >> 2][j & 3] * a.scale);
-                    e[t][j] = a.softcap * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + g));
-                }
-        } else {
-#pragma unroll
-            for (int t = 0; t < QT; ++t)
-#pragma unroll
-                for (int j = 0; j < kE; ++j) e[t][j] = z[t][j >> 2][j & 3] * a.scale;
+                for (int j = 0; j < kE; ++j)                                // cap tanh(x) with tanh x = 1 - 2 / (1 + exp 2x)
+                    e[t][j] = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(e[t][j] * a.scale)), 1.f);
+            by = a.softcap;
         }
-        const bool whole = key0 >= open0 && key0 + X::kKeys <= open1;
         uint32_t open[QT];
-        if (!whole) {
+        if constexpr (MASKED) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
                 open[t] = 0;
@@ -269,6 +255,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
             top[t] = e[t][0];
 #pragma unroll
             for (int j = 1; j < kE; ++j) top[t] = fmaxf(top[t], e[t][j]);
+            top[t] *= by;                                                   // by >= 0; 0 x inf is a NaN as it is in the scores
             move |= top[t] > m[t] + 8.f;
         }
         if (__builtin_amdgcn_ballot_w64(move) != 0) {
@@ -286,11 +273,11 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
         for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int j = 0; j < kE; ++j) {
-                e[t][j] = __builtin_amdgcn_exp2f(e[t][j] - m[t]);
-                if (!whole) e[t][j] = open[t] >> j & 1 ? e[t][j] : 0.f;
+                e[t][j] = __builtin_amdgcn_exp2f(fmaf(e[t][j], by, -m[t]));
+                if (MASKED) e[t][j] = open[t] >> j & 1 ? e[t][j] : 0.f;
                 l[t] += e[t][j];
             }
-        if (!whole) {
+        if constexpr (MASKED) {
             bool bad = false;
             const int behind = min(max(s.hi - (key0 + v_slot), 0), kE);                   // keys that exist
 #pragma unroll
@@ -308,7 +295,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
                 for (int key = 0; key < X::kKeys; ++key) {
                     if (key0 + key >= s.hi) break;
                     const int from = key / kE, j = key % kE;
-                    const T* src = v_pages + p.value_at(valid(__shfl(pv_now, 16 * from, 64)), kv, key0 + key);
+                    const T* src = v_pages + p.value_at(valid(__shfl(page, 16 * from, 64)), kv, key0 + key);
                     float w[QT];
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
@@ -346,12 +333,38 @@ __global__ __launch_bounds__(64 * kTreeWaves, QT == 4 || HD == 256 ? 1 : 2) void
 #pragma unroll
             for (int i = 0; i < kDims; ++i) o[t][i] = mma(vf[i], w, o[t][i]);
         }
-        if (more) {
-            pv = pv_next;
+    };
+
+    // Tiles that every row sees whole, [open0, open1) of them, lie in the middle; the masked ones at both ends come behind them, in a loop of their own:
+    // together the accumulators would move between the two kinds of registers in every round.
+    const int whole0 = min(max((s.L + s.n - a.window - s.lo + X::kKeys - 1) / X::kKeys * (a.window != 0), tile0), tile1);
+    const int whole1 = max(min((s.L - s.lo) / X::kKeys, tile1), whole0);
+    if (whole0 + wave < whole1) {
+        constexpr int kStride = kTreeWaves * X::kKeys;
+        int key0 = s.lo + (whole0 + wave) * X::kKeys;
+        int pk = page_at(key0 + k_slot), pv = page_at(key0 + v_slot), pk_next = page_at(key0 + kStride + k_slot), pv_next = page_at(key0 + kStride + v_slot);
+        load_keys(pk, key0);
+        load_values(pv, key0);
+        for (int tile = whole0 + wave; tile < whole1; tile += kTreeWaves) {
+            const bool more = tile + kTreeWaves < whole1;                   // if not, the same keys are read again, from the cache: no branch
+            const int next0 = more ? key0 + kStride : key0;
+            pk = more ? pk_next : pk;
+            pv = more ? pv_next : pv;
+            attend(std::false_type{}, key0, 0, [&] {
+                load_keys(pk, next0);
+                pk_next = page_at(next0 + kStride + k_slot);
+            });
             load_values(pv, next0);
-            pv_next = page_at(next0 + kTreeWaves * X::kKeys + v_slot);
+            pv_next = page_at(next0 + kStride + v_slot);
+            key0 = next0;
         }
-        key0 = next0;
+    }
+    const int before = whole0 - tile0, masked = before + tile1 - whole1;
+    for (int i = wave; i < masked; i += kTreeWaves) {
+        const int key0 = s.lo + (i < before ? tile0 + i : whole1 + i - before) * X::kKeys, page = page_at(key0 + v_slot);
+        load_keys(page_at(key0 + k_slot), key0);
+        load_values(page, key0);
+        attend(std::true_type{}, key0, page, [] {});
     }
 
     // The wavefronts together: references and sums first, then the outputs, 32 head elements at a time.
@@ -452,7 +465,7 @@ constexpr int64_t kTreePartRows = 1 << 16;                // (row, head, split) 
 TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max_rows, int32_t max_cached, int32_t window) {
     TreePlan t{};
     const int64_t rows = (int64_t)max_rows * (nq / c.n_kv_heads);
-    t.q_tiles = rows <= 16 ? 1 : rows <= 32 || c.head_dim > 128 ? 2 : 4;
+    t.q_tiles = rows <= 16 || c.head_dim > 128 ? 1 : rows <= 32 ? 2 : 3;      // 256 elements: the accumulators of 16 rows are what fits
     t.row_tiles = (int32_t)std::max<int64_t>(1, ceil_div(rows, 16 * t.q_tiles));
     const int64_t keys_per_tile = c.dtype == ATTS_DTYPE_F32 ? 16 : 32, slots = (int64_t)c.max_pages * c.page_rows;
     const auto splits_of = [&](int64_t context) {         // 256 keys or more each
@@ -487,17 +500,17 @@ int32_t launch_tree(const atts_paged_cache& c, const void* q, void* out, const P
 
 template <typename T>
 int32_t launch_tree_shape(const TreePlan& t, const atts_paged_cache& c, const void* q, void* out, const PagedView& p, const TreeArgs& a, hipStream_t stream) {
+    if (p.hd == 256) return launch_tree<T, 256, 1, true>(c, q, out, p, a, stream);
+    if (p.hd > 128) return launch_tree<T, 256, 1, false>(c, q, out, p, a, stream);
 #define ATTS_TREE(HD, EXACT)                                                                         \
     switch (t.q_tiles) {                                                                             \
         case 1: return launch_tree<T, HD, 1, EXACT>(c, q, out, p, a, stream);                        \
         case 2: return launch_tree<T, HD, 2, EXACT>(c, q, out, p, a, stream);                        \
-        default: return launch_tree<T, HD, (HD > 128 ? 2 : 4), EXACT>(c, q, out, p, a, stream);        \
+        default: return launch_tree<T, HD, 3, EXACT>(c, q, out, p, a, stream);                       \
     }
     if (p.hd == 64) { ATTS_TREE(64, true) }
     if (p.hd == 128) { ATTS_TREE(128, true) }
-    if (p.hd == 256) { ATTS_TREE(256, true) }
-    if (p.hd < 128) { ATTS_TREE(128, false) }
-    ATTS_TREE(256, false)
+    ATTS_TREE(128, false)
 #undef ATTS_TREE
 }
 
@@ -550,7 +563,7 @@ int32_t atts_attention_tree(const atts_paged_cache* cache, const void* q, const 
     // with a cap, scores enter tanh as 2 log2(e) scale / cap, and leave it in units of log2
     const float in = softcap > 0.f ? 2.f * kLog2e * scale / softcap : kLog2e * scale;
     const TreeArgs a{parents, cached, row_offsets, part_o, part_ml, R, n_q_heads, max_rows, max_cached, window, t.max_splits, t.tiles_per_split,
-                     t.row_tiles, (int32_t)groups, in, softcap * kLog2e};
+                     t.row_tiles, (int32_t)groups, scale < 0.f, fabsf(in), softcap * kLog2e};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (cache->dtype == ATTS_DTYPE_F32) return launch_tree_shape<float>(t, *cache, q, out, p, a, stream);
     return launch_tree_shape<bf16>(t, *cache, q, out, p, a, stream);
