@@ -30,6 +30,8 @@
 namespace atts {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kTreeWaves = 4;
 constexpr int kWords = ATTS_MAX_TREE / 32;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -73,15 +75,34 @@ __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
 }
 
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ bool any_not_finite(bf16x8 v) {
-    const auto u = __builtin_bit_cast(uint4, v);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    bool bad = false;
+// The first n elements, zeros behind them.
+__device__ __forceinline__ bf16x8 keep_first(bf16x8 v, int n) {
+    auto u = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-    return bad;
+    for (int i = 0; i < 4; ++i) u[i] &= n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xffffu : 0u;
+    return __builtin_bit_cast(bf16x8, u);
 }
-__device__ __forceinline__ bool any_not_finite(f32x4 v) { return not_finite(v[0]) || not_finite(v[1]) || not_finite(v[2]) || not_finite(v[3]); }
+__device__ __forceinline__ f32x4 keep_first(f32x4 v, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? v[i] : 0.f;
+    return v;
+}
+// The largest magnitudes so far as bits (bf16: in either half): those of infinities and NaNs are the largest of all.
+__device__ __forceinline__ uint32_t largest(uint32_t most, bf16x8 v) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const auto u = __builtin_bit_cast(u32x4, v);
+    u16x2 m = __builtin_bit_cast(u16x2, most);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, u[i] & 0x7fff7fffu));
+    return __builtin_bit_cast(uint32_t, m);
+}
+__device__ __forceinline__ uint32_t largest(uint32_t most, f32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+    return most;
+}
+__device__ __forceinline__ bool holds_not_finite(uint32_t most, bf16x8) { return (most & 0xffffu) >= 0x7f80u || most >= 0x7f800000u; }
+__device__ __forceinline__ bool holds_not_finite(uint32_t most, f32x4) { return most >= 0x7f800000u; }
 
 // HD: head_dim, or the next size up when EXACT is false; QT: tiles of 16 query rows.
 template <typename T, int HD, int QT, bool EXACT>
@@ -228,24 +249,27 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
                     e[t][j] = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(e[t][j] * a.scale)), 1.f);
             by = a.softcap;
         }
-        uint32_t open[QT];
+        uint32_t open[QT];                                                  // bit j: the row sees the lane's key j
         if constexpr (MASKED) {
+            // Of the lane's keys, the context's come first, then new rows from number `at` on (negative: context before them).
+            const int first = key0 + v_slot, at = first - s.L, exist = min(max(s.hi - first, 0), kE), context = min(max(-at, 0), kE);
+            const auto low = [](int n) { return (1u << n) - 1; };
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
-                open[t] = 0;
-#pragma unroll
-                for (int j = 0; j < kE; ++j) {
-                    const int key = key0 + v_slot + j, at = key - s.L;
-                    bool see = key < s.hi;
-                    int pos = key;
-                    if (see && at >= 0) {
-                        see = kin[own[t]][at >> 5] >> (at & 31) & 1;
-                        pos = s.L + depth[at];
-                    }
-                    if (see && a.window) see = s.L + depth[own[t]] - pos < a.window;
-                    open[t] |= (uint32_t)see << j;
-                    if (!see) e[t][j] = -INFINITY;
+                uint32_t see = low(context);
+                if (a.window) see &= ~low(min(max(s.L + depth[own[t]] - a.window + 1 - first, 0), kE));
+                if (at > -kE) {
+                    const int word = max(at, 0) >> 5;
+                    const uint64_t next = word + 1 < kWords ? kin[own[t]][word + 1] : 0u, two = next << 32 | (word < kWords ? kin[own[t]][word] : 0u);
+                    uint32_t tree = (uint32_t)(at >= 0 ? two >> (at & 31) : two << -at) & ~low(context);
+                    if (a.window && a.window < ATTS_MAX_TREE)               // narrow enough to part a tree
+                        for (int j = context; j < exist; ++j)
+                            if (depth[own[t]] - depth[at + j] >= a.window) tree &= ~(1u << j);
+                    see |= tree;
                 }
+                open[t] = see & low(exist);
+#pragma unroll
+                for (int j = 0; j < kE; ++j) e[t][j] = open[t] >> j & 1 ? e[t][j] : -INFINITY;
             }
         }
         float top[QT];
@@ -278,15 +302,15 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
                 l[t] += e[t][j];
             }
         if constexpr (MASKED) {
-            bool bad = false;
-            const int behind = min(max(s.hi - (key0 + v_slot), 0), kE);                   // keys that exist
+            if (key0 + X::kKeys > s.hi) {                                   // what lies behind the last key is anything
+                const int exist = min(max(s.hi - (key0 + v_slot), 0), kE);
 #pragma unroll
-            for (int i = 0; i < kDims; ++i) {
-#pragma unroll
-                for (int j = 0; j < kE; ++j) vf[i][j] = j < behind ? vf[i][j] : (T)0.f;
-                bad |= any_not_finite(vf[i]);
+                for (int i = 0; i < kDims; ++i) vf[i] = keep_first(vf[i], exist);
             }
-            if (__builtin_amdgcn_ballot_w64(bad) != 0) {
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < kDims; ++i) most = largest(most, vf[i]);
+            if (__builtin_amdgcn_ballot_w64(holds_not_finite(most, vf[0])) != 0) {
 #pragma unroll
                 for (int i = 0; i < kDims; ++i)
 #pragma unroll
@@ -367,25 +391,33 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
         attend(std::true_type{}, key0, page, [] {});
     }
 
-    // The wavefronts together: references and sums first, then the outputs, 32 head elements at a time.
+    // The wavefronts together: references and sums first, so that every one scales its own outputs, then these, 32 head elements at a time.
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         l[t] = row_sum(l[t]);
         if (c == 0) ml[wave][t * 16 + r] = make_float2(m[t], l[t]);
     }
     __syncthreads();
+    const bool alone = tiles <= a.tiles_per_split;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        float ref = -INFINITY;
+        float ref = -INFINITY, sum = 0.f;
 #pragma unroll
         for (int w = 0; w < kTreeWaves; ++w) ref = fmaxf(ref, ml[w][t * 16 + r].x);
-        const float keep = m[t] == ref ? 1.f : __builtin_amdgcn_exp2f(m[t] - ref);
+#pragma unroll
+        for (int w = 0; w < kTreeWaves; ++w) {
+            const float2 one = ml[w][t * 16 + r];
+            sum += one.x == ref ? one.y : one.y * __builtin_amdgcn_exp2f(one.x - ref);
+        }
+        float keep = m[t] == ref ? 1.f : __builtin_amdgcn_exp2f(m[t] - ref);
+        if (alone) keep = sum == 0.f ? 0.f : keep / sum;                    // no key at all: zeros
+        const int mq = row_tile * kRows + t * 16 + r;
+        if (!alone && wave == 0 && c == 0 && mq < n_rows)
+            a.part_ml[((int64_t)(s.first + own[t]) * a.nq + kv * group + mq % group) * a.max_splits + split] = make_float2(ref, sum);
 #pragma unroll
         for (int i = 0; i < kDims; ++i) o[t][i] *= keep;
     }
-    const bool alone = tiles <= a.tiles_per_split;
-    constexpr int kEach = kRows * 32 / (64 * kTreeWaves);           // elements a thread writes in a round
-    const int d_mine = tid & 31;
+    const int d_mine = (tid & 7) * 4;                                       // four elements of a row in 32 threads' rows at a time
 #pragma unroll
     for (int round = 0; round < kDims / 2; ++round) {
         __syncthreads();
@@ -394,25 +426,20 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
 #pragma unroll
             for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r][i * 16 + 4 * c]) = o[t][round * 2 + i];
         __syncthreads();
+        for (int row = tid >> 3; row < kRows; row += 32) {
+            const int mq = row_tile * kRows + row, d = round * 32 + d_mine;
+            if (mq >= n_rows || (!EXACT && d >= hd)) continue;              // hd is a multiple of 8
+            f32x4 y = *reinterpret_cast<const f32x4*>(&sums[0][row][d_mine]);
 #pragma unroll
-        for (int x = 0; x < kEach; ++x) {
-            const int row = (tid >> 5) + x * (2 * kTreeWaves), mq = row_tile * kRows + row, d = round * 32 + d_mine;
-            if (mq >= n_rows || (!EXACT && d >= hd)) continue;
-            float ref = -INFINITY, sum = 0.f, y = 0.f;
-#pragma unroll
-            for (int w = 0; w < kTreeWaves; ++w) ref = fmaxf(ref, ml[w][row].x);
-#pragma unroll
-            for (int w = 0; w < kTreeWaves; ++w) {
-                const float2 one = ml[w][row];
-                sum += one.x == ref ? one.y : one.y * __builtin_amdgcn_exp2f(one.x - ref);
-                y += sums[w][row][d_mine];
-            }
+            for (int w = 1; w < kTreeWaves; ++w) y += *reinterpret_cast<const f32x4*>(&sums[w][row][d_mine]);
             const int64_t at = (int64_t)(s.first + mq / group) * a.nq + kv * group + mq % group;
-            if (alone) out[at * hd + d] = from_f32<T>(sum == 0.f ? 0.f : y / sum);
-            else {
-                a.part_o[(at * a.max_splits + split) * hd + d] = y;
-                if (d == 0) a.part_ml[at * a.max_splits + split] = make_float2(ref, sum);
-            }
+            if (alone) {
+                typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));                 // outputs at any address
+                Four z;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) z[x] = from_f32<T>(y[x]);
+                *reinterpret_cast<Four*>(out + at * hd + d) = z;
+            } else *reinterpret_cast<f32x4*>(a.part_o + (at * a.max_splits + split) * hd + d) = y;
         }
     }
 }
