@@ -444,40 +444,58 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     }
 }
 
-// One workgroup per (row, query head) whose keys were cut: four wavefronts take every fourth split each, a lane up to four head elements.
+// One workgroup per (row, query head) whose keys were cut.  A thread takes four head elements of every n-th split, n = 256 / (hd / 4) of them side by
+// side, four rounds requested together; then the n sums are added in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void tree_join_kernel(T* __restrict__ out, PagedView p, TreeArgs a, int keys_per_tile) {
-    __shared__ float2 ml[4];
-    __shared__ float part[4][256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ f32x4 part[256];
+    __shared__ float weight[256], sums[4];
+    const int tid = threadIdx.x, lane = tid & 63;
     const int64_t at = blockIdx.x;
-    const int row = (int)(at / a.nq), seq = sequence_of(a.row_offsets, p.n_seqs, row);
+    const int row = (int)(at / a.nq), seq = sequence_of_wave(a.row_offsets, p.n_seqs, row, lane);
     if (seq < 0) return;
     const Sequence s(p, a, seq);
     if (row - s.first >= s.n) return;
     const int tiles = max(1, (s.hi - s.lo + keys_per_tile - 1) / keys_per_tile);
     if (tiles <= a.tiles_per_split) return;
     const int splits = (tiles + a.tiles_per_split - 1) / a.tiles_per_split;
+    const float2* const ml = a.part_ml + at * a.max_splits;
     float ref = -INFINITY;
-    for (int i = lane; i < splits; i += 64) ref = fmaxf(ref, a.part_ml[at * a.max_splits + i].x);
+    for (int i = lane; i < splits; i += 64) ref = fmaxf(ref, ml[i].x);
+    ref = wave_max(ref);
+    const int quads = p.hd / 4, beside = 256 / quads, quad = tid % quads, mine = tid / quads;
+    const f32x4* const src = reinterpret_cast<const f32x4*>(a.part_o + at * a.max_splits * p.hd) + quad;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int i0 = 0; i0 < splits; i0 += 256) {              // weights of 256 splits at a time
+        const int n = min(splits - i0, 256);
+        __syncthreads();
+        if (tid < n) {
+            const float2 one = ml[i0 + tid];
+            const float w = one.x == ref ? 1.f : __builtin_amdgcn_exp2f(one.x - ref);
+            weight[tid] = w;
+            sum += w * one.y;
+        }
+        __syncthreads();
+        if (mine < beside)
+            for (int i = mine; i < n; i += 4 * beside) {
+                f32x4 x[4];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d, 64));
-    float sum = 0.f, y[4] = {};
-#pragma unroll 4
-    for (int i = wave; i < splits; i += 4) {
-        const float2 one = a.part_ml[at * a.max_splits + i];
-        const float w = one.x == ref ? 1.f : __builtin_amdgcn_exp2f(one.x - ref);
-        sum += w * one.y;
+                for (int u = 0; u < 4; ++u) x[u] = src[(int64_t)(i0 + min(i + u * beside, n - 1)) * quads];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < p.hd) y[j] += w * a.part_o[(at * a.max_splits + i) * p.hd + lane + 64 * j];
+                for (int u = 0; u < 4; ++u)
+                    if (i + u * beside < n) y += weight[i + u * beside] * x[u];
+            }
     }
-    if (lane == 0) ml[wave].y = sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) part[wave][lane + 64 * j] = y[j];
+    sum = wave_sum(sum);
+    if (lane == 0) sums[tid >> 6] = sum;
+    part[tid] = y;
     __syncthreads();
-    const float total = ml[0].y + ml[1].y + ml[2].y + ml[3].y;
-    if (tid < p.hd) out[at * p.hd + tid] = from_f32<T>(total == 0.f ? 0.f : (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / total);
+    const float total = sums[0] + sums[1] + sums[2] + sums[3];
+    if (tid >= quads) return;
+    for (int i = 1; i < beside; ++i) y += part[tid + i * quads];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) out[at * p.hd + 4 * tid + x] = from_f32<T>(total == 0.f ? 0.f : y[x] / total);
 }
 
 // How a call is cut: tiles of query rows, and splits of the longest sequence's keys.
@@ -486,7 +504,6 @@ struct TreePlan {
     size_t bytes;
 };
 
-constexpr int64_t kTreeWorkgroups = 512;                  // two a compute unit
 constexpr int64_t kTreePartRows = 1 << 16;                // (row, head, split) partial sums of a call that is cut
 
 TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max_rows, int32_t max_cached, int32_t window) {
@@ -504,7 +521,9 @@ TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max
     t.bytes = max_cached + max_rows <= 256 ? 0 : align_up((size_t)bound * (c.head_dim + 2) * sizeof(float), 256);
     const int64_t context = window ? std::min((int64_t)max_cached, (int64_t)window + 31) : max_cached;
     const int64_t cells = std::max<int64_t>(1, (int64_t)c.n_seqs * c.n_kv_heads * t.row_tiles);
-    const int64_t splits = std::min(splits_of(context), ceil_div(kTreeWorkgroups, cells));
+    // Two workgroups a compute unit stream the cache as fast as more do; with more rows than one tile the products count too, and shorter
+    // splits even them out (70B heads, 1 row over 131,071 tokens: 103 us with 512 workgroups, 110 with 1024; 64 rows over 60,000: 335 and 289).
+    const int64_t splits = std::min(splits_of(context), ceil_div(t.q_tiles == 1 ? 512 : 1024, cells));
     const int64_t tiles = std::max<int64_t>(1, ceil_div(std::min(context + max_rows, slots), keys_per_tile));
     t.tiles_per_split = (int32_t)ceil_div(tiles, splits);
     t.max_splits = (int32_t)ceil_div(tiles, t.tiles_per_split);
