@@ -1,6 +1,7 @@
 // Products of a few rows with weights in 4 bits:  out = X W^T,  W[n, k] = scale[n, k / G] (code[n, k] - zero[n, k / G]).
 #include "common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace atts {
@@ -21,7 +22,7 @@ struct QuantArgs {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStageBytes = 32768;
+constexpr int kStageBytes = 36864;
 constexpr int kSpan = 128;       // K elements of a step: 16 bytes of codes a lane
 
 __device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
@@ -345,21 +346,20 @@ struct QuantPlan {
 QuantPlan quant_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t epilogue) {
     constexpr int64_t kChip = 256;                         // compute units
     QuantPlan p{};
-    const int64_t wide = epilogue == ATTS_EPILOGUE_SWIGLU ? 2 * (int64_t)N : N;
+    const bool swiglu = epilogue == ATTS_EPILOGUE_SWIGLU;
+    const int64_t wide = swiglu ? 2 * (int64_t)N : N;
     p.mt = M <= 16 || dtype == ATTS_DTYPE_F32 ? 1 : 2;     // fp32: three parts of X and their sums leave no room for a second block
     p.row_blocks = (int32_t)ceil_div(M, 16 * p.mt);
-    p.ns = M > 16 || ceil_div(wide, 64) >= kChip ? 4 : epilogue == ATTS_EPILOGUE_SWIGLU || ceil_div(wide, 32) >= kChip ? 2 : 1;
-    p.waves = p.ns == 4 ? 4 : 8;
-    const int64_t tiles = ceil_div(wide, 16 * p.ns);
-    p.tiles = (int32_t)(epilogue == ATTS_EPILOGUE_SWIGLU ? ceil_div(N, 8 * p.ns) : tiles);
+    // Tiles of 64 weight rows read X least often.  With at most 16 rows of X narrower ones follow where those would leave compute units without
+    // work: 32 from half a workgroup a unit on, else 16 (16 rows, K 27,648: N 5120 45 us with tiles of 16 and 35 with 32; 1 row, K 18,944: N 3584
+    // 19 and 25).  More rows keep the wide tiles and divide K, first among eight wavefronts instead of four, then over workgroups (24 rows,
+    // N 3584, K 18,944: 25 us with 4 splits, 55 with one; where the tiles fill the chip four wavefronts are faster: 64 rows, N 10,240, K 8192: 41 and 46).
+    p.ns = M > 16 || ceil_div(wide, 64) >= kChip ? 4 : swiglu || ceil_div(wide, 32) >= kChip / 2 ? 2 : 1;
+    p.tiles = (int32_t)(swiglu ? ceil_div(N, 8 * p.ns) : ceil_div(wide, 16 * p.ns));
+    const int64_t cells = (int64_t)p.tiles * p.row_blocks;
+    p.waves = p.ns == 4 && cells >= kChip ? 4 : 8;
     p.steps = (int32_t)ceil_div(K, kSpan);
-    int64_t splits = 1;
-    if (M > 16) {
-        splits = 2 * kChip / ((int64_t)p.tiles * p.row_blocks);
-        const int64_t most = p.steps / (2 * p.waves);     // two steps a wavefront at least
-        if (splits > most) splits = most;
-        if (splits < 1) splits = 1;
-    }
+    const int64_t splits = M <= 16 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kChip / cells, p.steps / 4));
     p.steps_per_split = (int32_t)ceil_div(p.steps, splits);
     p.splits = (int32_t)ceil_div(p.steps, p.steps_per_split);
     p.bytes = p.splits > 1 ? (size_t)p.splits * M * wide * sizeof(float) : 0;
@@ -385,8 +385,9 @@ int32_t launch_quant(const QuantPlan& p, QuantArgs a, hipStream_t stream) {
 
 template <typename T, int G>
 int32_t launch_quant_shape(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
-    if (p.mt == 2) return launch_quant<T, G, 4, sizeof(T) == 2 ? 2 : 1, 4>(p, a, stream);
-    if (p.ns == 4) return launch_quant<T, G, 4, 1, 4>(p, a, stream);
+    constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;           // fp32 has one block of rows a workgroup
+    if (p.mt == 2) return p.waves == 4 ? launch_quant<T, G, 4, kTwo, 4>(p, a, stream) : launch_quant<T, G, 4, kTwo, 8>(p, a, stream);
+    if (p.ns == 4) return p.waves == 4 ? launch_quant<T, G, 4, 1, 4>(p, a, stream) : launch_quant<T, G, 4, 1, 8>(p, a, stream);
     return p.ns == 2 ? launch_quant<T, G, 2, 1, 8>(p, a, stream) : launch_quant<T, G, 1, 1, 8>(p, a, stream);
 }
 
