@@ -1,0 +1,196 @@
+"""Greedy decoding of several requests with drafted token trees: one step of the target model verifies a whole tree a request.
+
+    python examples/tree_decode.py
+
+A decoder of the family that the library scores (synthetic weights), its projections in 4 bits, its keys and values in a paged cache.  Every step:
+4-bit products, rotary append, tree attention and logits adjustment for the rows of all requests together; then the longest path of every tree that
+agrees with the model's own choices is kept, its cache entries are moved together, and the choice behind it starts the next tree.  The tokens are
+those of decoding one token a step, whatever the drafts.
+"""
+from __future__ import annotations
+
+import math
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2509_15148_amd as A
+from synth import ModelConfig, make_weights
+
+GROUP = 32
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class QuantMatrix:
+    """A weight matrix as codes, scales and zeros."""
+
+    def __init__(self, w: torch.Tensor):
+        n, k = w.shape
+        self.rows = n
+        self.codes = torch.empty(n, k // 2, dtype=torch.uint8, device="cuda")
+        self.scales = torch.empty(n, k // GROUP, dtype=w.dtype, device="cuda")
+        self.zeros = torch.empty(n, k // GROUP, dtype=torch.uint8, device="cuda")
+        A.atts_quantize_rows(w.cuda().contiguous(), self.codes, self.scales, self.zeros)
+
+    def __call__(self, x: torch.Tensor, epilogue: int = A.EPILOGUE_STORE, residual=None) -> torch.Tensor:
+        n = self.rows // 2 if epilogue == A.EPILOGUE_SWIGLU else self.rows
+        wide = epilogue in (A.EPILOGUE_RESIDUAL, A.EPILOGUE_STORE_F32)
+        out = residual if residual is not None else torch.empty(x.shape[0], n, dtype=torch.float32 if wide else x.dtype, device="cuda")
+        A.atts_gemm_nt_quant(x, self.codes, self.scales, self.zeros, out, epilogue, residual)
+        return out
+
+
+class TreeDecoder:
+    """The target model over a paged cache for `n_seqs` requests of at most `capacity` tokens each."""
+
+    def __init__(self, cfg: ModelConfig, weights, n_seqs: int, capacity: int, page_rows: int = 16):
+        self.cfg, self.dtype = cfg, cfg.torch_dtype
+        self.embed, self.final_norm, self.lm_head = (weights[k].cuda() for k in ("tok_embed", "final_norm", "lm_head"))
+        self.layers = [dict(attn_norm=weights["attn_norm"][l].cuda(), ffn_norm=weights["ffn_norm"][l].cuda(), qkv=QuantMatrix(weights["wqkv"][l]),
+                            o=QuantMatrix(weights["wo"][l]), gate_up=QuantMatrix(weights["w_gate_up"][l]), down=QuantMatrix(weights["w_down"][l]))
+                       for l in range(cfg.n_layers)]
+        pages = -(-capacity // page_rows)
+        self.page_rows, self.capacity = page_rows, pages * page_rows
+        self.table = torch.randperm(n_seqs * pages, generator=torch.Generator().manual_seed(1)).to(torch.int32).reshape(n_seqs, pages).cuda()
+        shape = (n_seqs * pages, cfg.n_kv_heads)
+        self.caches = [A.PagedCache(torch.zeros(*shape, page_rows, cfg.head_dim, dtype=self.dtype, device="cuda"),
+                                    torch.zeros(*shape, cfg.head_dim, page_rows, dtype=self.dtype, device="cuda"), self.table) for _ in self.layers]
+        self.rotary = torch.empty(self.capacity, cfg.head_dim // 2, 2, device="cuda")
+        A.atts_rotary_table(self.rotary, cfg.rope_theta)
+        self.cached = [0] * n_seqs
+
+    def _norm(self, h, gain):
+        return (h * torch.rsqrt((h * h).mean(dim=1, keepdim=True) + self.cfg.rms_eps) * gain).to(self.dtype)
+
+    def step(self, tokens, parents):
+        """tokens, parents: one list of rows a request (possibly empty).  -> logits [rows, vocab] behind every row; nothing is kept of the rows
+        but their keys and values, behind `cached`."""
+        cfg, lens = self.cfg, [len(t) for t in tokens]
+        flat = [t for row in tokens for t in row]
+        offsets = [0]
+        for n in lens:
+            offsets.append(offsets[-1] + n)
+        positions = []
+        for c, tree in zip(self.cached, parents):
+            depth = []
+            for p in tree:
+                depth.append(depth[p] + 1 if p >= 0 else 0)
+            positions += [c + d for d in depth]
+        R, most = len(flat), max(lens)
+        pos, cached, off, par = _i32(positions), _i32(self.cached), _i32(offsets), _i32([p for tree in parents for p in tree])
+        nq, hd = cfg.n_q_heads, cfg.head_dim
+        h = self.embed[_i32(flat).long()].float()
+        q, attended = (torch.empty(R, nq * hd, dtype=self.dtype, device="cuda") for _ in range(2))
+        space = torch.empty(max(256, A.atts_attention_tree_workspace_bytes(self.caches[0], nq, R, most, max(self.cached))), dtype=torch.uint8, device="cuda")
+        for w, cache in zip(self.layers, self.caches):
+            qkv = w["qkv"](self._norm(h, w["attn_norm"]))
+            A.atts_rotary_append(cache, qkv, pos, cached, off, self.rotary, A.ROTARY_HALF, q)
+            A.atts_attention_tree(cache, q, par, cached, off, most, max(self.cached), attended, space)
+            w["o"](attended, A.EPILOGUE_RESIDUAL, h)
+            w["down"](w["gate_up"](self._norm(h, w["ffn_norm"]), A.EPILOGUE_SWIGLU), A.EPILOGUE_RESIDUAL, h)
+        logits = torch.empty(R, cfg.vocab, device="cuda")
+        A.atts_gemm_nt(self._norm(h, self.final_norm), self.lm_head, logits)
+        return logits
+
+    def keep(self, paths):
+        """Of every request's new rows, those of `path` (ascending) become the context."""
+        for s, path in enumerate(paths):
+            old = [self.cached[s] + i for i in path]
+            new = [self.cached[s] + i for i in range(len(path))]
+            if old != new:
+                at = lambda tokens: (self.table[s, [t // self.page_rows for t in tokens]].long(), torch.tensor([t % self.page_rows for t in tokens], device="cuda"))
+                (p0, s0), (p1, s1) = at(old), at(new)
+                for cache in self.caches:
+                    cache.k_pages[p1, :, s1] = cache.k_pages[p0, :, s0]
+                    cache.v_pages[p1, :, :, s1] = cache.v_pages[p0, :, :, s0]
+            self.cached[s] += len(path)
+
+
+def choose(logits, tokens, parents, history, prompt_lens, params):
+    """The model's choice behind every row under the requests' rules: its own path counts as generated."""
+    R, V = logits.shape
+    lens = [len(t) for t in tokens]
+    offsets = lambda n: _i32([sum(n[:i]) for i in range(len(n) + 1)])
+    top, lse = torch.empty(R, dtype=torch.int32, device="cuda"), torch.empty(R, device="cuda")
+    space = torch.empty(max(256, A.atts_logits_adjust_workspace_bytes(R, V)), dtype=torch.uint8, device="cuda")
+    A.atts_logits_adjust(logits, offsets(lens), params, _i32([t for h in history for t in h]), offsets([len(h) for h in history]), _i32(prompt_lens),
+                         _i32([t for row in tokens for t in row]), _i32([p for tree in parents for p in tree]), None, None, None, None, logits, top, lse,
+                         space, max_rows=max(lens))
+    chosen, out = top.tolist(), []
+    for n in lens:
+        out.append(chosen[:n])
+        chosen = chosen[n:]
+    return out
+
+
+def longest_agreed(tokens, parents, chosen):
+    """Rows of the longest path whose every token is the choice behind the row before it; row 0, the token already decided, begins it."""
+    path, at = [0], 0
+    while True:
+        following = [i for i, p in enumerate(parents) if p == at and tokens[i] == chosen[at]]
+        if not following:
+            return path
+        at = following[0]
+        path.append(at)
+
+
+def decode(model: TreeDecoder, prompts, n_new: int, params, draft):
+    """n_new tokens for every prompt.  draft(tokens so far) -> (tokens, parents) of a tree that may follow them.  -> tokens, steps of the model"""
+    steps = 0
+    for s, prompt in enumerate(prompts):                       # prompts in chains as long as a tree may be; the last token starts the first tree
+        for first in range(0, len(prompt) - 1, 256):
+            part = prompt[first:min(first + 256, len(prompt) - 1)]
+            own = lambda x: [x if i == s else [] for i in range(len(prompts))]
+            model.step(own(part), own(list(range(-1, len(part) - 1))))
+            model.keep(own(list(range(len(part)))))
+    made, pending = [[] for _ in prompts], [p[-1] for p in prompts]
+    while min(len(m) for m in made) < n_new:
+        trees = []
+        for p, m, last in zip(prompts, made, pending):
+            tokens, parents = draft(p + m)
+            trees.append(([last] + tokens, [-1] + [q + 1 for q in parents]))
+        tokens, parents = [t[0] for t in trees], [t[1] for t in trees]
+        # the pending token is the history's last entry and the tree's first row: it is counted once, by the row
+        history = [(p + m)[:-1] for p, m in zip(prompts, made)]
+        chosen = choose(model.step(tokens, parents), tokens, parents, history, [len(p) - 1 if not m else len(p) for p, m in zip(prompts, made)], params)
+        paths = [longest_agreed(t, p, c) for t, p, c in zip(tokens, parents, chosen)]
+        for s, path in enumerate(paths):
+            made[s] += [tokens[s][i] for i in path[1:]] + [chosen[s][path[-1]]]
+            pending[s] = made[s][-1]
+        model.keep(paths)
+        steps += 1
+    return [m[:n_new] for m in made], steps
+
+
+def main():
+    cfg = ModelConfig(2, 128, 4, 4, 32, 512, 1024, "fp32")
+    weights = make_weights(cfg, seed=11, device="cuda")
+    gen = torch.Generator().manual_seed(3)
+    prompts = [torch.randint(0, cfg.vocab, (n,), generator=gen).tolist() for n in (300, 1, 17)]
+    params = torch.tensor([[1.1, 0.2, 0.1, 0.9]] * len(prompts), device="cuda")
+    n_new = 24
+
+    def run(draft):
+        model = TreeDecoder(cfg, weights, len(prompts), capacity=300 + n_new + 40)
+        return decode(model, [list(p) for p in prompts], n_new, params, draft)
+    plain, steps = run(lambda so_far: ([], []))
+    print(f"one token a step: {steps} steps")
+    known = [p + t for p, t in zip(prompts, plain)]
+
+    def draft(so_far):
+        """Two branches of three tokens: one right for its first two tokens, one wrong from its first."""
+        full = next((k for k in known if k[:len(so_far)] == so_far), so_far)
+        right = (full[len(so_far):] + [0, 0, 0])[:3]
+        return right[:2] + [(right[2] + 1) % cfg.vocab] + [(right[0] + 5) % cfg.vocab, 1, 2], [-1, 0, 1, -1, 3, 4]
+    trees, steps = run(draft)
+    print(f"trees of 7 rows: {steps} steps, same tokens: {trees == plain}")
+    return plain, trees
+
+
+if __name__ == "__main__":
+    main()
