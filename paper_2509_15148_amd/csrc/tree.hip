@@ -35,6 +35,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTreeWaves = 4;
 constexpr int kWords = ATTS_MAX_TREE / 32;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;               // references begin here: a score of -inf weighs nothing, also where nothing else came before it
 
 struct TreeArgs {
     const int32_t *parents, *cached, *row_offsets;
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     float m[QT], l[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        m[t] = -INFINITY;
+        m[t] = kLowest;
         l[t] = 0.f;
 #pragma unroll
         for (int i = 0; i < kDims; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
