@@ -1,24 +1,28 @@
 // Attention of drafted token trees over a paged key / value cache.
 //
 // For a sequence with L cached tokens and n new rows, group = n_q / n_kv query heads share a key / value head: its n group query rows all read
-// the same cached keys, and every row also reads the new rows it descends from.  A step reads each key and value once for a handful of
-// rows, so what bounds it is the cache's bytes: the kernel is built to keep loads in flight, straight from HBM into the registers that feed the matrix
-// cores, with no LDS and no barrier inside the loop.
+// the same cached keys, and every row also reads the new rows it descends from.  z = scale q.k (or cap tanh(z / cap)), out = sum exp(z) v / sum exp(z)
+// in one pass over the keys, with a running maximum.  A few rows over a long context are bound by the cache's bytes (one row of 70B heads over 131,071
+// tokens: 100 us, 5.3 TB/s, the rate of a large copy); many rows by the vector unit, which takes an exponential a score, two with a cap (24 sequences of
+// 32B heads, up to 64 rows, cap and window: 161 us, 0.35 PFLOP/s); a single tree by the way of one workgroup from its first load to its last
+// barrier (16 rows of 7B heads over 512 tokens: 10.7 us).
 //
-//   * A wavefront holds up to 64 query rows (tiles of 16) and walks over tiles of 32 keys (16 in fp32).  S^T = K Q^T: the keys are the rows of the
+//   * A wavefront holds up to 48 query rows (tiles of 16) and walks over tiles of 32 keys (16 in fp32).  S^T = K Q^T: the keys are the rows of the
 //     product, so lane (r = l % 16, c = l / 16) ends with scores of query row r only, of 8 (4) keys that lie one behind the other.  These are just
 //     the B operand of O^T = V^T P^T: the probabilities go from the accumulators into the next product without leaving their lane.
-//     Which key is which row of the first product is free, it is chosen so; the values are transposed in the cache, so their operand too is one
-//     16-byte load a lane.
-//   * The keys of the next tile are requested when the scores of this one are done, its values when they are used up: one set of registers, always
-//     one of the two under way.  Page numbers are read two tiles ahead.
+//     Which key is which row of the first product is free, it is chosen so; the values are transposed in the cache, so theirs is the same.
+//   * Memory is read four lanes a 64-byte piece of a row, and LDS turns rows into fragments, 16 bytes a lane either way, with no barrier: a wavefront turns
+//     its own.  Fragments loaded as the matrix cores take them, 16 rows side by side, pass at a quarter of the rate (one row, 7B heads, 2040 tokens in
+//     one workgroup: 27 us, so 19).
+//   * The next tile's keys are requested when these are in LDS, its values likewise: one set of registers, always one of the two under way.  Page
+//     numbers are read a tile ahead of them.
 //   * exp2 with a reference that moves only when a score passes it by 8 (a probability is then at most 2^8): per tile one ballot instead of a
 //     reduction over lanes; sums stay in their lanes until the end.  bf16: probabilities are rounded to 16 bits for the second product, the
 //     matrix cores take nothing wider beside 16-bit values; their sum is of the unrounded ones.
 //   * Only tiles at a window's edge and those of the tree are masked.  There a lane checks its values: those that are not finite are taken out of the
 //     product (0 x NaN would reach every row) and added by themselves to the rows that see them.
-//   * The four wavefronts of a workgroup take every fourth tile and are joined through LDS; a long context is cut over workgroups
-//     (tree_plan), whose partial sums a second launch joins in their order.
+//   * The wavefronts of a workgroup take tiles in turn and are joined through LDS; a long context is cut over workgroups (tree_plan), whose
+//     partial sums a second launch joins in their order.
 #include "lanes.h"
 #include "paged.h"
 
@@ -32,7 +36,9 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTreeWaves = 4;
+// Wavefronts of a workgroup: eight shorten the way over a few hundred keys (70B heads, 4 x 16 rows, 4090 tokens: 41 us, 54 with four); with more rows a
+// wavefront they cost more to join than they gain (24 sequences of 32B heads, 8 rows, up to 600 tokens: 26 us with four, 33 with eight).
+constexpr int tree_waves(int q_tiles) { return q_tiles == 1 ? 8 : 4; }
 constexpr int kWords = ATTS_MAX_TREE / 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;               // references begin here: a score of -inf weighs nothing, also where nothing else came before it
@@ -107,15 +113,19 @@ __device__ __forceinline__ bool holds_not_finite(uint32_t most, f32x4) { return 
 
 // HD: head_dim, or the next size up when EXACT is false; QT: tiles of 16 query rows.
 template <typename T, int HD, int QT, bool EXACT>
-__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
+__global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
         const T* __restrict__ q, const T* __restrict__ k_pages, const T* __restrict__ v_pages, T* __restrict__ out, PagedView p, TreeArgs a) {
     using X = Shape<T>;
     using Vec = typename X::Vec;
-    constexpr int kSteps = HD / X::kStep, kDims = HD / 16, kE = X::kLaneKeys, kRows = 16 * QT, kPitch = 36;
+    constexpr int kSteps = HD / X::kStep, kDims = HD / 16, kE = X::kLaneKeys, kRows = 16 * QT, kPitch = 36, kWaves = tree_waves(QT);
     __shared__ uint32_t kin[ATTS_MAX_TREE][kWords];       // bit j of row i: row j is row i or an ancestor of it
     __shared__ int16_t depth[ATTS_MAX_TREE];
-    __shared__ float2 ml[kTreeWaves][kRows];
-    __shared__ float sums[kTreeWaves][kRows][kPitch];
+    __shared__ float2 ml[kWaves][kRows];
+    // fragments of a tile on their way, behind the loop sums
+    constexpr int kTurn = (X::kSub * kSteps > kDims ? X::kSub * kSteps : kDims) * 64, kSums = kRows * kPitch;
+    __shared__ __attribute__((aligned(16))) char shared[kWaves * (kTurn * 16 > kSums * 4 ? kTurn * 16 : kSums * 4)];
+    Vec (*const turn)[kTurn] = reinterpret_cast<Vec (*)[kTurn]>(shared);
+    float (*const sums)[kRows][kPitch] = reinterpret_cast<float (*)[kRows][kPitch]>(shared);
 
     // Workgroups that read the same keys lie 8 apart, which is the same XCD and so the same L2.
     const int id = blockIdx.x, row_tile = id / 8 % a.row_tiles, grp = id / (8 * a.row_tiles) * 8 + id % 8;
@@ -189,7 +199,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
         __syncthreads();
     }
     // Key rows of the first product: lane row r of sub-tile u is key 8 (r / 4) + 4 u + r % 4 (bf16), key r (fp32).
-    const int k_slot = X::kSub == 2 ? 8 * (r >> 2) + (r & 3) : r, v_slot = kE * c;
+    // Memory is read in rows, four lanes 64 bytes: lanes of 16 different rows in a row would take a cycle each.  So lane l loads quarter l % 4 of
+    // row l / 4, and LDS turns that into a fragment, quarter l / 16 of row l % 16; a wavefront's accesses are done in their order, nothing waits for them.
+    const int rr = lane >> 2, quarter = lane & 3;
+    const int k_slot = X::kSub == 2 ? 8 * (rr >> 2) + (rr & 3) : rr, v_load = kE * quarter, v_slot = kE * c;
+    Vec* const to = turn[wave] + (lane & ~3) + (quarter ^ (lane >> 3 & 3));
+    const Vec* const from = turn[wave] + r * 4 + (c ^ (r >> 1 & 3));
     auto page_at = [&](int token) {
         const int at = min(token >> p.page_log, p.max_pages - 1);
         return p.table[(int64_t)seq * p.max_pages + at];
@@ -202,18 +217,20 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
         for (int u = 0; u < X::kSub; ++u)
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const int d = i * X::kStep + c * X::kElems;
+                const int d = i * X::kStep + quarter * X::kElems;
                 if (EXACT || d < hd) kf[u][i] = *reinterpret_cast<const Vec*>(src + u * 4 * hd + d);
                 else kf[u][i] = Vec{};
             }
     };
     auto load_values = [&](int page, int key0) __attribute__((always_inline)) {
-        const T* src = v_pages + p.value_at(valid(page), kv, key0 + v_slot);
+        // one address a lane and steps that all lanes share; of a head that ends inside, rows behind the end are read as its last
+        const T* src = v_pages + p.value_at(valid(page), kv, key0 + v_load);
+        const int end = EXACT ? HD : (hd - 1) & ~15;                        // first row of the last fragment that holds any
+        const T* const tail = src + ((int64_t)min(rr, hd - 1 - end) << p.page_log);
+        src += (int64_t)rr << p.page_log;
 #pragma unroll
-        for (int i = 0; i < kDims; ++i) {
-            const int d = i * 16 + r;
-            vf[i] = *reinterpret_cast<const Vec*>(src + ((int64_t)(EXACT ? d : min(d, hd - 1)) << p.page_log));
-        }
+        for (int i = 0; i < kDims; ++i)
+            vf[i] = *reinterpret_cast<const Vec*>((EXACT || i * 16 < end ? src : tail) + ((int64_t)(EXACT ? i * 16 : min(i * 16, end)) << p.page_log));
     };
 
     f32x4 o[QT][kDims];
@@ -227,20 +244,33 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     }
 
     // One tile of keys, in kf and vf; `refill` requests the next keys once these are used.  MASKED: some row may not see some key.
-    auto attend = [&](auto masked, int key0, int page, auto&& refill) __attribute__((always_inline)) {
+    auto attend = [&](auto masked, int key0, int page, auto&& refill, auto&& refill_values) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked)::value;
         float e[QT][kE];
 #pragma unroll
+        for (int u = 0; u < X::kSub; ++u)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) to[(u * kSteps + i) * 64] = kf[u][i];
+        refill();
+        f32x4 z[QT][X::kSub];
+        int q_lane = lane;
+        asm volatile("" : "+v"(q_lane));                                    // the queries are read again for every tile, not kept in registers
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            Vec key[X::kSub];
+#pragma unroll
+            for (int u = 0; u < X::kSub; ++u) key[u] = from[(u * kSteps + i) * 64];
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const Vec query = kQueriesInLds ? lds_q[(t * kSteps + i) * 64 + q_lane] : qf[kQueriesInLds ? 0 : t][i];
+#pragma unroll
+                for (int u = 0; u < X::kSub; ++u) z[t][u] = mma(key[u], query, i ? z[t][u] : f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+        }
+#pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int u = 0; u < X::kSub; ++u) {
-                f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) z = mma(kf[u][i], kQueriesInLds ? lds_q[(t * kSteps + i) * 64 + lane] : qf[kQueriesInLds ? 0 : t][i], z);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) e[t][u * 4 + x] = z[x];
-            }
-        refill();
+            for (int j = 0; j < kE; ++j) e[t][j] = z[t][j >> 2][j & 3];
         float by = a.scale;                                                 // what turns e into units of log2
         if (a.softcap > 0.f) {
 #pragma unroll
@@ -302,34 +332,45 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
                 if (MASKED) e[t][j] = open[t] >> j & 1 ? e[t][j] : 0.f;
                 l[t] += e[t][j];
             }
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) to[i * 64] = vf[i];
+        refill_values();
+        Vec w[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int j = 0; j < kE; ++j) w[t][j] = (T)e[t][j];
+        Vec vt[MASKED ? kDims : 1];
         if constexpr (MASKED) {
+#pragma unroll
+            for (int i = 0; i < kDims; ++i) vt[i] = from[i * 64];
             if (key0 + X::kKeys > s.hi) {                                   // what lies behind the last key is anything
                 const int exist = min(max(s.hi - (key0 + v_slot), 0), kE);
 #pragma unroll
-                for (int i = 0; i < kDims; ++i) vf[i] = keep_first(vf[i], exist);
+                for (int i = 0; i < kDims; ++i) vt[i] = keep_first(vt[i], exist);
             }
             uint32_t most = 0;
 #pragma unroll
-            for (int i = 0; i < kDims; ++i) most = largest(most, vf[i]);
-            if (__builtin_amdgcn_ballot_w64(holds_not_finite(most, vf[0])) != 0) {
+            for (int i = 0; i < kDims; ++i) most = largest(most, vt[i]);
+            if (__builtin_amdgcn_ballot_w64(holds_not_finite(most, vt[0])) != 0) {
 #pragma unroll
                 for (int i = 0; i < kDims; ++i)
 #pragma unroll
-                    for (int j = 0; j < kE; ++j) vf[i][j] = not_finite((float)vf[i][j]) ? (T)0.f : vf[i][j];
+                    for (int j = 0; j < kE; ++j) vt[i][j] = not_finite((float)vt[i][j]) ? (T)0.f : vt[i][j];
 #pragma unroll 1
                 for (int key = 0; key < X::kKeys; ++key) {
                     if (key0 + key >= s.hi) break;
-                    const int from = key / kE, j = key % kE;
-                    const T* src = v_pages + p.value_at(valid(__shfl(page, 16 * from, 64)), kv, key0 + key);
-                    float w[QT];
+                    const int at = key / kE, j = key % kE;
+                    const T* src = v_pages + p.value_at(valid(__shfl(page, at, 64)), kv, key0 + key);
+                    float weight[QT];
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
                         float mine = e[t][0];
 #pragma unroll
                         for (int x = 1; x < kE; ++x) mine = x == j ? e[t][x] : mine;
-                        const bool sees = __shfl((int)open[t], r + 16 * from, 64) >> j & 1;
-                        mine = __shfl(mine, r + 16 * from, 64);
-                        w[t] = sees ? mine : -1.f;                                        // a probability is never negative
+                        const bool sees = __shfl((int)open[t], r + 16 * at, 64) >> j & 1;
+                        mine = __shfl(mine, r + 16 * at, 64);
+                        weight[t] = sees ? mine : -1.f;                                   // a probability is never negative
                     }
                     src += (int64_t)(4 * c) << p.page_log;
 #pragma unroll
@@ -340,7 +381,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
                             if (not_finite(v)) {
 #pragma unroll
                                 for (int t = 0; t < QT; ++t)
-                                    if (!(w[t] < 0.f)) o[t][i][x] += w[t] * v;
+                                    if (!(weight[t] < 0.f)) o[t][i][x] += weight[t] * v;
                             }
                             src += (int64_t)1 << p.page_log;
                             asm volatile("" : "+v"(src));              // one address that moves on, not 4 kDims kept in registers
@@ -351,12 +392,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
             }
         }
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            Vec w;
+        for (int i = 0; i < kDims; ++i) {
+            const Vec value = MASKED ? vt[MASKED ? i : 0] : from[i * 64];
 #pragma unroll
-            for (int j = 0; j < kE; ++j) w[j] = (T)e[t][j];
-#pragma unroll
-            for (int i = 0; i < kDims; ++i) o[t][i] = mma(vf[i], w, o[t][i]);
+            for (int t = 0; t < QT; ++t) o[t][i] = mma(value, w[t], o[t][i]);
         }
     };
 
@@ -365,31 +404,32 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     const int whole0 = min(max((s.L + s.n - a.window - s.lo + X::kKeys - 1) / X::kKeys * (a.window != 0), tile0), tile1);
     const int whole1 = max(min((s.L - s.lo) / X::kKeys, tile1), whole0);
     if (whole0 + wave < whole1) {
-        constexpr int kStride = kTreeWaves * X::kKeys;
+        constexpr int kStride = kWaves * X::kKeys;
         int key0 = s.lo + (whole0 + wave) * X::kKeys;
-        int pk = page_at(key0 + k_slot), pv = page_at(key0 + v_slot), pk_next = page_at(key0 + kStride + k_slot), pv_next = page_at(key0 + kStride + v_slot);
+        int pk = page_at(key0 + k_slot), pv = page_at(key0 + v_load), pk_next = page_at(key0 + kStride + k_slot), pv_next = page_at(key0 + kStride + v_load);
         load_keys(pk, key0);
         load_values(pv, key0);
-        for (int tile = whole0 + wave; tile < whole1; tile += kTreeWaves) {
-            const bool more = tile + kTreeWaves < whole1;                   // if not, the same keys are read again, from the cache: no branch
+        for (int tile = whole0 + wave; tile < whole1; tile += kWaves) {
+            const bool more = tile + kWaves < whole1;                   // if not, the same keys are read again, from the cache: no branch
             const int next0 = more ? key0 + kStride : key0;
             pk = more ? pk_next : pk;
             pv = more ? pv_next : pv;
             attend(std::false_type{}, key0, 0, [&] {
                 load_keys(pk, next0);
                 pk_next = page_at(next0 + kStride + k_slot);
+            }, [&] {
+                load_values(pv, next0);
+                pv_next = page_at(next0 + kStride + v_load);
             });
-            load_values(pv, next0);
-            pv_next = page_at(next0 + kStride + v_slot);
             key0 = next0;
         }
     }
     const int before = whole0 - tile0, masked = before + tile1 - whole1;
-    for (int i = wave; i < masked; i += kTreeWaves) {
-        const int key0 = s.lo + (i < before ? tile0 + i : whole1 + i - before) * X::kKeys, page = page_at(key0 + v_slot);
+    for (int i = wave; i < masked; i += kWaves) {
+        const int key0 = s.lo + (i < before ? tile0 + i : whole1 + i - before) * X::kKeys, page = page_at(key0 + v_load);
         load_keys(page_at(key0 + k_slot), key0);
         load_values(page, key0);
-        attend(std::true_type{}, key0, page, [] {});
+        attend(std::true_type{}, key0, page, [] {}, [] {});
     }
 
     // The wavefronts together: references and sums first, so that every one scales its own outputs, then these, 32 head elements at a time.
@@ -404,9 +444,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     for (int t = 0; t < QT; ++t) {
         float ref = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) ref = fmaxf(ref, ml[w][t * 16 + r].x);
+        for (int w = 0; w < kWaves; ++w) ref = fmaxf(ref, ml[w][t * 16 + r].x);
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
             const float2 one = ml[w][t * 16 + r];
             sum += one.x == ref ? one.y : one.y * __builtin_amdgcn_exp2f(one.x - ref);
         }
@@ -427,12 +467,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
 #pragma unroll
             for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r][i * 16 + 4 * c]) = o[t][round * 2 + i];
         __syncthreads();
-        for (int row = tid >> 3; row < kRows; row += 32) {
+        for (int row = tid >> 3; row < kRows; row += 8 * kWaves) {
             const int mq = row_tile * kRows + row, d = round * 32 + d_mine;
             if (mq >= n_rows || (!EXACT && d >= hd)) continue;              // hd is a multiple of 8
             f32x4 y = *reinterpret_cast<const f32x4*>(&sums[0][row][d_mine]);
 #pragma unroll
-            for (int w = 1; w < kTreeWaves; ++w) y += *reinterpret_cast<const f32x4*>(&sums[w][row][d_mine]);
+            for (int w = 1; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(&sums[w][row][d_mine]);
             const int64_t at = (int64_t)(s.first + mq / group) * a.nq + kv * group + mq % group;
             if (alone) {
                 typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));                 // outputs at any address
@@ -445,10 +485,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attention_kernel(
     }
 }
 
-// One workgroup per (row, query head) whose keys were cut.  A thread takes four head elements of every n-th split, n = 256 / (hd / 4) of them side by
+// More than kFew splits: one workgroup per (row, query head) whose keys were cut.  A thread takes four head elements of every n-th split, n = 256 / (hd / 4) of them side by
 // side, four rounds requested together; then the n sums are added in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void tree_join_kernel(T* __restrict__ out, PagedView p, TreeArgs a, int keys_per_tile) {
+__global__ __launch_bounds__(256) void tree_join_many_kernel(T* __restrict__ out, PagedView p, TreeArgs a, int keys_per_tile) {
     __shared__ f32x4 part[256];
     __shared__ float weight[256], sums[4];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -499,6 +539,48 @@ __global__ __launch_bounds__(256) void tree_join_kernel(T* __restrict__ out, Pag
     for (int x = 0; x < 4; ++x) out[at * p.hd + 4 * tid + x] = from_f32<T>(total == 0.f ? 0.f : y[x] / total);
 }
 
+// Up to kFew splits: hd / 4 threads a (row, query head), several of these a workgroup; a thread takes four head elements of every split, requested
+// together (70B heads, 4 x 16 rows, 2 splits: 19 us both launches, 24 with a workgroup each).
+constexpr int kFew = 8;
+template <typename T>
+__global__ __launch_bounds__(256) void tree_join_few_kernel(T* __restrict__ out, PagedView p, TreeArgs a, int keys_per_tile) {
+    const int tid = threadIdx.x, lane = tid & 63, quads = p.hd / 4, beside = 256 / quads, quad = tid % quads;
+    const int64_t last = (int64_t)a.R * a.nq - 1, at0 = (int64_t)blockIdx.x * beside, mine = at0 + tid / quads, at = min(mine, last);
+    // the rows of a wavefront lie one behind the other, mostly they are one
+    const int row = (int)(at / a.nq), row0 = __builtin_amdgcn_readfirstlane(row), row1 = __builtin_amdgcn_readlane(row, 63);
+    int splits = 0;
+    for (int x = row0; x <= row1; ++x) {
+        const int seq = sequence_of_wave(a.row_offsets, p.n_seqs, x, lane);
+        if (seq < 0) continue;
+        const Sequence s(p, a, seq);
+        const int tiles = max(1, (s.hi - s.lo + keys_per_tile - 1) / keys_per_tile);
+        if (x - s.first < s.n && tiles > a.tiles_per_split && row == x) splits = (tiles + a.tiles_per_split - 1) / a.tiles_per_split;
+    }
+    if (mine > last || tid >= beside * quads || splits == 0) return;
+    const float2* const ml = a.part_ml + at * a.max_splits;
+    const f32x4* const src = reinterpret_cast<const f32x4*>(a.part_o + at * a.max_splits * p.hd) + quad;
+    float2 one[kFew];
+    f32x4 x[kFew];
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) {
+        one[i] = ml[min(i, splits - 1)];
+        x[i] = src[(int64_t)min(i, splits - 1) * quads];
+    }
+    float ref = one[0].x, sum = 0.f;
+#pragma unroll
+    for (int i = 1; i < kFew; ++i) ref = fmaxf(ref, one[i].x);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kFew; ++i)
+        if (i < splits) {
+            const float w = one[i].x == ref ? 1.f : __builtin_amdgcn_exp2f(one[i].x - ref);
+            sum += w * one[i].y;
+            y += w * x[i];
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[at * p.hd + 4 * quad + i] = from_f32<T>(sum == 0.f ? 0.f : y[i] / sum);
+}
+
 // How a call is cut: tiles of query rows, and splits of the longest sequence's keys.
 struct TreePlan {
     int32_t q_tiles, row_tiles, tiles_per_split, max_splits;
@@ -507,27 +589,32 @@ struct TreePlan {
 
 constexpr int64_t kTreePartRows = 1 << 16;                // (row, head, split) partial sums of a call that is cut
 
+// Keys that one workgroup takes faster than several do with the launch that joins them: 7B heads, 4 rows, 1020 tokens: 12.4 us, 13.1 in splits; 2040
+// tokens: 17.8 and 13.0.
+constexpr int64_t kTreeWhole = 1024;
+
 TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max_rows, int32_t max_cached, int32_t window) {
+    constexpr int64_t kChip = 256;                        // compute units
     TreePlan t{};
-    const int64_t rows = (int64_t)max_rows * (nq / c.n_kv_heads);
-    t.q_tiles = rows <= 16 || c.head_dim > 128 ? 1 : rows <= 32 ? 2 : 3;      // 256 elements: the accumulators of 16 rows are what fits
-    t.row_tiles = (int32_t)std::max<int64_t>(1, ceil_div(rows, 16 * t.q_tiles));
+    const int64_t rows = (int64_t)max_rows * (nq / c.n_kv_heads), heads = (int64_t)c.n_seqs * c.n_kv_heads;
     const int64_t keys_per_tile = c.dtype == ATTS_DTYPE_F32 ? 16 : 32, slots = (int64_t)c.max_pages * c.page_rows;
-    const auto splits_of = [&](int64_t context) {         // 256 keys or more each
-        const int64_t keys = std::min(context + max_rows, slots);
-        return std::max<int64_t>(1, std::min(ceil_div(keys, 256), kTreePartRows / std::max<int64_t>(1, (int64_t)R * nq)));
-    };
-    // the bound of the workspace does not know the window, and grows with every argument
-    const int64_t bound = std::min((int64_t)R * nq * ceil_div(std::min((int64_t)max_cached + max_rows, slots), 256), kTreePartRows);
-    t.bytes = max_cached + max_rows <= 256 ? 0 : align_up((size_t)bound * (c.head_dim + 2) * sizeof(float), 256);
-    const int64_t context = window ? std::min((int64_t)max_cached, (int64_t)window + 31) : max_cached;
-    const int64_t cells = std::max<int64_t>(1, (int64_t)c.n_seqs * c.n_kv_heads * t.row_tiles);
-    // Two workgroups a compute unit stream the cache as fast as more do; with more rows than one tile the products count too, and shorter
-    // splits even them out (70B heads, 1 row over 131,071 tokens: 103 us with 512 workgroups, 110 with 1024; 64 rows over 60,000: 335 and 289).
-    const int64_t splits = std::min(splits_of(context), ceil_div(t.q_tiles == 1 ? 512 : 1024, cells));
-    const int64_t tiles = std::max<int64_t>(1, ceil_div(std::min(context + max_rows, slots), keys_per_tile));
+    const int64_t keys = std::min((window ? std::min((int64_t)max_cached, (int64_t)window + 31) : max_cached) + (int64_t)max_rows, slots);
+    // Row tiles of 48 read the cache a third as often as tiles of 16, whose shorter way is faster while each finds a compute unit of its own (7B heads,
+    // 16 rows, 520 tokens: 10.9 us with 16 and 16.2 with 48; 70B heads, 4 x 16 rows, 4090 tokens: 32 and 39, 30,000 tokens: 192 and 109; 32B heads,
+    // 4 x 32 rows, 1.25 tiles of 16 a unit, 4090 tokens: 57 and 35).  Heads of 256: the accumulators of 16 rows are what fits.
+    t.q_tiles = rows <= 16 || c.head_dim > 128 || (keys <= 4096 && heads * ceil_div(rows, 16) <= kChip) ? 1 : rows <= 32 ? 2 : 3;
+    t.row_tiles = (int32_t)std::max<int64_t>(1, ceil_div(rows, 16 * t.q_tiles));
+    // Splits fill what the compute units hold at a time, one workgroup of eight wavefronts or two of four, and not more (70B heads, 64 rows, 60,000 tokens,
+    // 88 tiles: 215 us with 5 splits and 258 with 6), of 256 keys or more.
+    const int64_t room = (t.q_tiles == 1 ? kChip : 2 * kChip) / std::max<int64_t>(1, heads * t.row_tiles);
+    const int64_t most = std::min(ceil_div(keys, 256), kTreePartRows / std::max<int64_t>(1, (int64_t)R * nq));
+    const int64_t splits = keys <= kTreeWhole ? 1 : std::max<int64_t>(1, std::min(room, most));
+    const int64_t tiles = std::max<int64_t>(1, ceil_div(keys, keys_per_tile));
     t.tiles_per_split = (int32_t)ceil_div(tiles, splits);
     t.max_splits = (int32_t)ceil_div(tiles, t.tiles_per_split);
+    // the bound of the workspace knows neither the window nor the other sequences, and grows with every argument
+    const int64_t bound = std::min((int64_t)R * nq * ceil_div(std::min((int64_t)max_cached + max_rows, slots), 256), kTreePartRows);
+    t.bytes = max_cached + (int64_t)max_rows <= kTreeWhole ? 0 : align_up((size_t)bound * (c.head_dim + 2) * sizeof(float), 256);
     return t;
 }
 
@@ -535,12 +622,18 @@ template <typename T, int HD, int QT, bool EXACT>
 int32_t launch_tree(const atts_paged_cache& c, const void* q, void* out, const PagedView& p, const TreeArgs& a, hipStream_t stream) {
     const int64_t wgs = ceil_div(a.n_groups, 8) * 8 * a.row_tiles;
     if (wgs > 0x7fffffff) return fail(ATTS_ERR_SHAPE, "atts_attention_tree: the call has more than 2^31 workgroups");
-    hipLaunchKernelGGL((tree_attention_kernel<T, HD, QT, EXACT>), dim3((unsigned)wgs), dim3(64 * kTreeWaves), 0, stream, static_cast<const T*>(q),
+    hipLaunchKernelGGL((tree_attention_kernel<T, HD, QT, EXACT>), dim3((unsigned)wgs), dim3(64 * tree_waves(QT)), 0, stream, static_cast<const T*>(q),
                        static_cast<const T*>(c.k_pages), static_cast<const T*>(c.v_pages), static_cast<T*>(out), p, a);
     ATTS_LAUNCH_CHECK("tree_attention_kernel");
     if (a.max_splits > 1) {
-        hipLaunchKernelGGL(tree_join_kernel<T>, dim3((unsigned)((int64_t)a.R * a.nq)), dim3(256), 0, stream, static_cast<T*>(out), p, a, Shape<T>::kKeys);
-        ATTS_LAUNCH_CHECK("tree_join_kernel");
+        const int64_t outs = (int64_t)a.R * a.nq;
+        if (a.max_splits <= kFew) {
+            hipLaunchKernelGGL(tree_join_few_kernel<T>, dim3((unsigned)ceil_div(outs, 256 / (p.hd / 4))), dim3(256), 0, stream, static_cast<T*>(out), p, a, Shape<T>::kKeys);
+            ATTS_LAUNCH_CHECK("tree_join_few_kernel");
+        } else {
+            hipLaunchKernelGGL(tree_join_many_kernel<T>, dim3((unsigned)outs), dim3(256), 0, stream, static_cast<T*>(out), p, a, Shape<T>::kKeys);
+            ATTS_LAUNCH_CHECK("tree_join_many_kernel");
+        }
     }
     return ATTS_OK;
 }
@@ -557,6 +650,7 @@ int32_t launch_tree_shape(const TreePlan& t, const atts_paged_cache& c, const vo
     }
     if (p.hd == 64) { ATTS_TREE(64, true) }
     if (p.hd == 128) { ATTS_TREE(128, true) }
+    if (p.hd < 64) { ATTS_TREE(64, false) }
     ATTS_TREE(128, false)
 #undef ATTS_TREE
 }
