@@ -1,6 +1,12 @@
 // The logits of a step under their requests' rules: penalties for tokens that came before, sparse biases, temperature, a grammar mask;
 // with the first arg max and the log-sum-exp of the result.
 //
+// x = z / rep (z > 0) or z rep for a token of the prompt, the generated text or the row's path; x - count frequency - presence for what was generated;
+// x + bias; x / temperature; -inf where the mask is 0: each rounded by itself, so that the result is that of the steps.  It has to read and write every
+// logit once.  One row is bound by two launches (152,064 logits, 9.3 us); many rows by the vector unit, at 20 to 35 instructions a token and 16 more in
+// the pieces that hold a token of the history, which with thousands of those is nearly every one (16 trees, 144 rows of 152,064 in 32 bits: 63 us, 2.8 TB/s;
+// 256 rows of 128,256 in 16 bits with histories of up to 32,000: 73 us, 2.1 TB/s; a copy of as many bytes takes 45 and 26).
+//
 //   * A workgroup takes a slice of the vocabulary for the rows of one sequence.  How often each token of the slice came before is
 //     counted into LDS from the history (integer atomics: the order does not matter), once for all rows.  The tokens of a row's own path in the tree are
 //     counted before its turn and taken out behind it, which for nearly all rows and slices is nothing at all.  Nothing of the size of
@@ -8,7 +14,7 @@
 //   * The logits of the next row are requested before those of this one are used; results stay in registers for the maximum and the sum of
 //     exponentials: one read and one write of the logits.  Every wavefront leaves (maximum, its index, sum) of its part; a second launch joins the
 //     parts of a row in a fixed order.
-//   * Slices of 4096 tokens fill the chip with few rows; slices of 16,384 read a long history a quarter as often (logits_plan).
+//   * Slices of 1024 (16 bits: 2048) tokens spread a few rows, of 4096 more; slices of 16,384 or 32,768 read a long history less often (logits_plan).
 #include "lanes.h"
 #include "paged.h"
 
@@ -19,7 +25,8 @@
 namespace atts {
 namespace {
 
-constexpr int kTokens = 16;      // of a thread
+constexpr int kTokens = 16;      // of a thread in a round
+template <typename T> constexpr int kShort = 16 / sizeof(T);               // the same with few rows: one load
 
 struct Part {
     float top, sum;          // maximum, sum of exp(x - top); top = -inf: nothing above -inf
@@ -109,10 +116,10 @@ __device__ __forceinline__ T element(const typename Load<T, VEC>::Raw& v, int i)
     else return v[i];
 }
 
-// VEC consecutive tokens at a time (16 bytes), or 1 where addresses or V do not allow it; a slice takes PASSES rounds of kTokens a thread.
-template <typename T, int VEC, int THREADS, int PASSES>
+// VEC consecutive tokens at a time (16 bytes), or 1 where addresses or V do not allow it; a slice takes PASSES rounds of TOKENS a thread.
+template <typename T, int VEC, int THREADS, int PASSES, int TOKENS>
 __global__ __launch_bounds__(THREADS, 4) void logits_kernel(const T* logits, T* out, const LogitsArgs a) {
-    constexpr int kRound = THREADS * kTokens, kSlice = kRound * PASSES, kLoads = kTokens / VEC;
+    constexpr int kRound = THREADS * TOKENS, kSlice = kRound * PASSES, kLoads = TOKENS / VEC;
     typedef typename Load<T, VEC>::Raw Raw;
     extern __shared__ __attribute__((aligned(16))) uint32_t smem[];
     uint32_t* const seen = smem;                         // [kSlice + 64] how often a token came before, none: 0
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(THREADS, 4) void logits_kernel(const T* logits, T* 
         load(next, min(item + 1, items - 1));
         if (paths) count_path(row, 1u);
         T* const dst = out + r * a.out_stride + v0;
-        float x[kTokens], most[kLoads], top = -INFINITY;
+        float x[TOKENS], most[kLoads], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int at = place(round, i);
@@ -285,10 +292,10 @@ __global__ __launch_bounds__(THREADS, 4) void logits_kernel(const T* logits, T* 
             float sum = 0.f;
             if (fabsf(best) < INFINITY) {
 #pragma unroll
-                for (int i = 0; i < kTokens; ++i) sum += __builtin_amdgcn_exp2f((x[i] - best) * 1.4426950408889634f);
+                for (int i = 0; i < TOKENS; ++i) sum += __builtin_amdgcn_exp2f((x[i] - best) * 1.4426950408889634f);
             } else {                                        // nothing above -inf, or +inf: NaNs stay NaN, the others count if they are the maximum +inf
 #pragma unroll
-                for (int i = 0; i < kTokens; ++i) sum += isnan(x[i]) ? x[i] : x[i] == INFINITY ? 1.f : 0.f;
+                for (int i = 0; i < TOKENS; ++i) sum += isnan(x[i]) ? x[i] : x[i] == INFINITY ? 1.f : 0.f;
             }
             sum = wave_sum(sum);
             uint32_t lowest = ~0u;                          // the first piece that holds the maximum, in any lane, has its lowest index
@@ -314,9 +321,13 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const Part* __restrict_
     const int seq = sequence_of_wave(row_offsets, n_seqs, r, lane);
     if (seq < 0 || r - row_offsets[seq] >= max_rows || row_offsets[seq] < 0) return;
     Part p{-INFINITY, 0.f, -1, 0};
-    for (int i = lane; i < n_parts; i += 64) {
-        const Part o = parts[(int64_t)r * n_parts + i];
-        join(p, o.top, o.id, o.sum);
+    for (int i = lane; i < n_parts; i += 4 * 64) {                     // four requested together
+        Part o[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u] = parts[(int64_t)r * n_parts + min(i + u * 64, n_parts - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * 64 < n_parts) join(p, o[u].top, o[u].id, o[u].sum);
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) {
@@ -331,12 +342,28 @@ __global__ __launch_bounds__(64) void logits_join_kernel(const Part* __restrict_
 
 // Threads of a workgroup, rounds and slices of the vocabulary, rows of a workgroup.
 struct LogitsPlan {
-    int32_t threads, passes, slices, rows_per_wg;
+    int32_t threads, passes, tokens, slices, rows_per_wg;
 };
 
-LogitsPlan logits_plan(int32_t n_seqs, int32_t max_rows, int32_t V, bool counts, bool bias) {
+// With so few rows and slices of 256 kTokens that compute units would have no work, a thread takes one load's tokens instead (152,064 logits in 32 bits, a
+// history of 2000: 1 row 9.4 us and 10.9 with kTokens, 4 rows 10.6 and 11.2, 8 rows, 304 slices, 12.8 and 12.4).
+constexpr int64_t kFewSlices = 256;
+bool logits_short(int64_t R, int32_t V) { return R * ceil_div(V, 256 * kTokens) <= kFewSlices; }
+
+LogitsPlan logits_plan(int32_t dtype, int32_t R, int32_t n_seqs, int32_t max_rows, int32_t V, int32_t n_history, bool counts, bool bias) {
     LogitsPlan p;
-    p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 ? 1024 : 256;
+    if (logits_short(R, V)) {
+        p.threads = 256;
+        p.passes = p.rows_per_wg = 1;
+        p.tokens = 16 / (int32_t)dtype_size(dtype);
+        p.slices = (int32_t)ceil_div(V, 256 * p.tokens);
+        return p;
+    }
+    p.tokens = kTokens;
+    // Every slice reads the whole history: with many sequences of long ones larger slices cost less than what smaller ones gain by running side by side
+    // (128,256 logits in 16 bits, 256 rows, histories of 16,000 on average: 74 us with slices of 32,768, 81 with 16,384, 93 with 4096; 152,064 logits in 32
+    // bits, 256 rows: 105, 119 and 130, with histories of 1000 91, 100 and 83; 64 x 4 rows, histories of 4000: 97, 90 and 82).
+    p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 && n_history / n_seqs >= 8192 ? 1024 : 256;
     p.passes = p.threads == 1024 && counts && !bias ? 2 : 1;                  // with biases too, two rounds' tables do not fit the LDS
     p.slices = (int32_t)ceil_div(V, p.threads * kTokens * p.passes);
     const int64_t cells = (int64_t)n_seqs * p.slices, chunks = std::min<int64_t>(max_rows, std::max<int64_t>(1, 1536 / std::max<int64_t>(1, cells)));
@@ -344,13 +371,13 @@ LogitsPlan logits_plan(int32_t n_seqs, int32_t max_rows, int32_t V, bool counts,
     return p;
 }
 
-template <typename T, int VEC, int THREADS, int PASSES>
+template <typename T, int VEC, int THREADS, int PASSES, int TOKENS>
 int32_t launch_logits(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
-    constexpr size_t table = (size_t)THREADS * kTokens * PASSES * 4;
+    constexpr size_t table = (size_t)THREADS * TOKENS * PASSES * 4;
     constexpr bool both = 2 * table <= 160 * 1024 - 4096;
-    const int32_t rc = allow_dynamic_lds<logits_kernel<T, VEC, THREADS, PASSES>>((both ? 2 * table : table) + 256);
+    const int32_t rc = allow_dynamic_lds<logits_kernel<T, VEC, THREADS, PASSES, TOKENS>>((both ? 2 * table : table) + 256);
     if (rc != ATTS_OK) return rc;
-    hipLaunchKernelGGL((logits_kernel<T, VEC, THREADS, PASSES>), dim3((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs),
+    hipLaunchKernelGGL((logits_kernel<T, VEC, THREADS, PASSES, TOKENS>), dim3((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs),
                        dim3(THREADS), (a.params ? table + 256 : 0) + (a.bias_ids ? table : 0), stream, static_cast<const T*>(logits), static_cast<T*>(out), a);
     ATTS_LAUNCH_CHECK("logits_kernel");
     return ATTS_OK;
@@ -358,8 +385,10 @@ int32_t launch_logits(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, 
 
 template <typename T, int VEC>
 int32_t launch_logits_shape(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
-    if (p.threads == 256) return launch_logits<T, VEC, 256, 1>(p, a, n_seqs, logits, out, stream);
-    return p.passes == 2 ? launch_logits<T, VEC, 1024, 2>(p, a, n_seqs, logits, out, stream) : launch_logits<T, VEC, 1024, 1>(p, a, n_seqs, logits, out, stream);
+    if (p.tokens == kShort<T>) return launch_logits<T, VEC, 256, 1, kShort<T>>(p, a, n_seqs, logits, out, stream);
+    if (p.threads == 256) return launch_logits<T, VEC, 256, 1, kTokens>(p, a, n_seqs, logits, out, stream);
+    return p.passes == 2 ? launch_logits<T, VEC, 1024, 2, kTokens>(p, a, n_seqs, logits, out, stream)
+                         : launch_logits<T, VEC, 1024, 1, kTokens>(p, a, n_seqs, logits, out, stream);
 }
 
 template <typename T>
@@ -380,7 +409,9 @@ int32_t atts_logits_adjust_workspace_bytes(int32_t R, int32_t V, size_t* out_byt
     const char* fn = "atts_logits_adjust_workspace_bytes";
     if (!out_bytes) return fail(ATTS_ERR_INVALID_ARG, "%s: out_bytes is NULL", fn);
     if (R < 0 || R > (1 << 24) || V < 1 || V > (1 << 30)) return fail(ATTS_ERR_INVALID_ARG, "%s: R outside [0, 2^24] or V outside [1, 2^30]", fn);
-    *out_bytes = align_up((size_t)R * ceil_div(V, 2048 * kTokens) * 32 * sizeof(Part), 256);      // a part for every wavefront, whichever the slices
+    // a part for every wavefront, whichever the slices, growing with both arguments: short slices have up to four times the parts of the others
+    const int64_t parts = (int64_t)R * ceil_div(V, 2048 * kTokens) * 32, shorts = std::min((int64_t)R * ceil_div(V, 256 * 4) * 4, kFewSlices * 16);
+    *out_bytes = align_up((size_t)std::max(parts, shorts) * sizeof(Part), 256);
     return ATTS_OK;
 }
 
@@ -407,7 +438,7 @@ int32_t atts_logits_adjust(int32_t dtype, const void* logits, int64_t logits_str
     const bool decide = top_ids || lse;
     if (decide && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need))
         return fail(ATTS_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", fn, need);
-    const LogitsPlan p = logits_plan(n_seqs, max_rows, V, params != nullptr, bias_ids != nullptr);
+    const LogitsPlan p = logits_plan(dtype, R, n_seqs, max_rows, V, n_history, params != nullptr, bias_ids != nullptr);
     const LogitsArgs a{row_offsets, params, history, history_offsets, prompt_lens, tree_ids, parents, bias_ids, bias_offsets, bias_values, mask,
                        decide ? static_cast<Part*>(workspace) : nullptr, logits_stride, out_stride, ceil_div(V, 32), max_rows, n_history, n_bias, R, V,
                        p.slices * p.passes * (p.threads / 64), p.rows_per_wg};

@@ -37,6 +37,14 @@ def test_many_sequences_of_logits(dtype, V, n_seqs, bias):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,bias", [(130000, 0), (130001, 0), (130000, 3), (130001, 3)])
+def test_many_long_histories(dtype, V, bias):
+    announce("logits long histories", dtype, V, bias)
+    c = Case(V, [1 + s % 2 for s in range(33)], [9000 - 10 * s for s in range(33)], dtype, bias=bias, mask=V % 2 == 0, seed=V)
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("M", [17, 32, 33, 70])
 @pytest.mark.parametrize("N,K,group,epilogue", [(64, 4096, 32, "store"), (200, 2048, 128, "swiglu"), (1100, 768, 64, "residual"), (8300, 256, 32, "store_f32")])
 @pytest.mark.parametrize("dtype", DTYPES)
