@@ -117,7 +117,8 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
         const T* __restrict__ q, const T* __restrict__ k_pages, const T* __restrict__ v_pages, T* __restrict__ out, PagedView p, TreeArgs a) {
     using X = Shape<T>;
     using Vec = typename X::Vec;
-    constexpr int kSteps = HD / X::kStep, kDims = HD / 16, kE = X::kLaneKeys, kRows = 16 * QT, kPitch = 36, kWaves = tree_waves(QT);
+    constexpr int kSteps = HD / X::kStep, kDims = HD / 16, kE = X::kLaneKeys, kRows = 16 * QT, kWaves = tree_waves(QT);
+    constexpr int kRound = QT == 3 && HD > 64 ? 128 / (int)sizeof(T) : HD, kPitch = kRound + 4;             // head elements that are joined at a time
     __shared__ uint32_t kin[ATTS_MAX_TREE][kWords];       // bit j of row i: row j is row i or an ancestor of it
     __shared__ int16_t depth[ATTS_MAX_TREE];
     __shared__ float2 ml[kWaves][kRows];
@@ -140,6 +141,7 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, c = lane >> 4;
     const bool tree_here = s.lo + tile1 * X::kKeys > s.L || a.window != 0;
 
+    int up = tree_here && tid < s.n ? a.parents[s.first + tid] : -1;
     // Queries: in registers, or, 64 rows, in LDS, fragment by fragment as the lanes take them: with them the accumulators would not fit the
     // registers that the vector unit reaches, and move to and fro.
     constexpr bool kQueriesInLds = QT > 2;
@@ -162,42 +164,6 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
         }
     }
     if (kQueriesInLds) __syncthreads();
-    if (tree_here) {
-        int up = -1;
-        if (tid < s.n) {
-            up = a.parents[s.first + tid];
-            if (up < 0 || up >= tid) up = -1;
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) kin[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
-            depth[tid] = (int16_t)up;
-        }
-        __syncthreads();
-        // every round doubles the ancestors a row knows; depth holds how far up it has looked
-        for (int reach = 1; reach < s.n; reach *= 2) {
-            uint32_t more[kWords] = {};
-            int next = -1;
-            if (up >= 0) {
-#pragma unroll
-                for (int w = 0; w < kWords; ++w) more[w] = kin[up][w];
-                next = depth[up];
-            }
-            __syncthreads();
-            if (up >= 0) {
-#pragma unroll
-                for (int w = 0; w < kWords; ++w) kin[tid][w] |= more[w];
-                depth[tid] = (int16_t)next;
-            }
-            up = next;
-            __syncthreads();
-        }
-        if (tid < s.n) {
-            int above = -1;
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) above += __popc(kin[tid][w]);
-            depth[tid] = (int16_t)above;
-        }
-        __syncthreads();
-    }
     // Key rows of the first product: lane row r of sub-tile u is key 8 (r / 4) + 4 u + r % 4 (bf16), key r (fp32).
     // Memory is read in rows, four lanes 64 bytes: lanes of 16 different rows in a row would take a cycle each.  So lane l loads quarter l % 4 of
     // row l / 4, and LDS turns that into a fragment, quarter l / 16 of row l % 16; a wavefront's accesses are done in their order, nothing waits for them.
@@ -233,6 +199,56 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
             vf[i] = *reinterpret_cast<const Vec*>((EXACT || i * 16 < end ? src : tail) + ((int64_t)(EXACT ? i * 16 : min(i * 16, end)) << p.page_log));
     };
 
+    // Tiles that every row sees whole, [whole0, whole1) of them, lie in the middle; the masked ones at both ends come behind them, in a loop of their own:
+    // together the accumulators would move between the two kinds of registers in every round.  Wavefronts take whole tiles, then masked ones in turn.
+    const int whole0 = min(max((s.L + s.n - a.window - s.lo + X::kKeys - 1) / X::kKeys * (a.window != 0), tile0), tile1);
+    const int whole1 = max(min((s.L - s.lo) / X::kKeys, tile1), whole0);
+    const int before = whole0 - tile0, masked = before + tile1 - whole1, first_masked = (wave + kWaves - (whole1 - whole0) % kWaves) % kWaves;
+    constexpr int kStride = kWaves * X::kKeys;
+    if (tree_here) {
+        if (tid < s.n) {
+            if (up < 0 || up >= tid) up = -1;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) kin[tid][w] = w == tid >> 5 ? 1u << (tid & 31) : 0u;
+            depth[tid] = (int16_t)up;
+        }
+        __syncthreads();
+        // every round doubles the ancestors a row knows; depth holds how far up it has looked
+        for (int reach = 1; reach < s.n; reach *= 2) {
+            uint32_t more[kWords] = {};
+            int next = -1;
+            if (up >= 0) {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) more[w] = kin[up][w];
+                next = depth[up];
+            }
+            __syncthreads();
+            if (up >= 0) {
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) kin[tid][w] |= more[w];
+                depth[tid] = (int16_t)next;
+            }
+            up = next;
+            __syncthreads();
+        }
+        if (tid < s.n) {
+            int above = -1;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) above += __popc(kin[tid][w]);
+            depth[tid] = (int16_t)above;
+        }
+        __syncthreads();
+    }
+    const bool some = whole0 + wave < whole1;
+    int key0 = s.lo + (whole0 + wave) * X::kKeys, pk = 0, pv = 0, pk_next = 0, pv_next = 0;
+    if (some) {
+        pk = page_at(key0 + k_slot);
+        pv = page_at(key0 + v_load);
+        pk_next = page_at(key0 + kStride + k_slot);
+        pv_next = page_at(key0 + kStride + v_load);
+        load_keys(pk, key0);
+        load_values(pv, key0);
+    }
     f32x4 o[QT][kDims];
     float m[QT], l[QT];
 #pragma unroll
@@ -399,16 +415,7 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
         }
     };
 
-    // Tiles that every row sees whole, [open0, open1) of them, lie in the middle; the masked ones at both ends come behind them, in a loop of their own:
-    // together the accumulators would move between the two kinds of registers in every round.
-    const int whole0 = min(max((s.L + s.n - a.window - s.lo + X::kKeys - 1) / X::kKeys * (a.window != 0), tile0), tile1);
-    const int whole1 = max(min((s.L - s.lo) / X::kKeys, tile1), whole0);
-    if (whole0 + wave < whole1) {
-        constexpr int kStride = kWaves * X::kKeys;
-        int key0 = s.lo + (whole0 + wave) * X::kKeys;
-        int pk = page_at(key0 + k_slot), pv = page_at(key0 + v_load), pk_next = page_at(key0 + kStride + k_slot), pv_next = page_at(key0 + kStride + v_load);
-        load_keys(pk, key0);
-        load_values(pv, key0);
+    if (some) {
         for (int tile = whole0 + wave; tile < whole1; tile += kWaves) {
             const bool more = tile + kWaves < whole1;                   // if not, the same keys are read again, from the cache: no branch
             const int next0 = more ? key0 + kStride : key0;
@@ -424,8 +431,7 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
             key0 = next0;
         }
     }
-    const int before = whole0 - tile0, masked = before + tile1 - whole1;
-    for (int i = wave; i < masked; i += kWaves) {
+    for (int i = first_masked; i < masked; i += kWaves) {
         const int key0 = s.lo + (i < before ? tile0 + i : whole1 + i - before) * X::kKeys, page = page_at(key0 + v_load);
         load_keys(page_at(key0 + k_slot), key0);
         load_values(page, key0);
@@ -458,17 +464,16 @@ __global__ __launch_bounds__(64 * tree_waves(QT), 2) void tree_attention_kernel(
 #pragma unroll
         for (int i = 0; i < kDims; ++i) o[t][i] *= keep;
     }
-    const int d_mine = (tid & 7) * 4;                                       // four elements of a row in 32 threads' rows at a time
 #pragma unroll
-    for (int round = 0; round < kDims / 2; ++round) {
+    for (int round = 0; round < HD / kRound; ++round) {
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r][i * 16 + 4 * c]) = o[t][round * 2 + i];
+            for (int i = 0; i < kRound / 16; ++i) *reinterpret_cast<f32x4*>(&sums[wave][t * 16 + r][i * 16 + 4 * c]) = o[t][round * (kRound / 16) + i];
         __syncthreads();
-        for (int row = tid >> 3; row < kRows; row += 8 * kWaves) {
-            const int mq = row_tile * kRows + row, d = round * 32 + d_mine;
+        for (int item = tid; item < kRows * kRound / 4; item += 64 * kWaves) {
+            const int row = item / (kRound / 4), d_mine = item % (kRound / 4) * 4, mq = row_tile * kRows + row, d = round * kRound + d_mine;
             if (mq >= n_rows || (!EXACT && d >= hd)) continue;              // hd is a multiple of 8
             f32x4 y = *reinterpret_cast<const f32x4*>(&sums[0][row][d_mine]);
 #pragma unroll
