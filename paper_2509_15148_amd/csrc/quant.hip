@@ -1,4 +1,15 @@
 // Products of a few rows with weights in 4 bits:  out = X W^T,  W[n, k] = scale[n, k / G] (code[n, k] - zero[n, k / G]).
+//
+// A group's sum is scale (sum_k (16 + code) x - (16 + zero) sum_k x): 16 + code is exact in 16 bits and costs one shift and one and-or for two codes, so
+// the matrix cores multiply codes with activations exactly, their product with a column of ones gives sum_k x, and the scale, 32 bits, comes once a
+// group.  In 32 bits x goes in as three 16-bit parts whose sum it is.  Every weight has to be read once, half a byte and its share of a scale; up to 16 rows
+// that is the bound (2 x 28,672 rows of W, K 8192, 16 rows, SwiGLU: 63 us, 3.9 TB/s, 78 % of a copy's rate; 4608 x 3584, one row: 6.6 us, an append of
+// a few rows takes 5.7).  With more rows the vector unit is: unpacking, the groups' multiply-adds and moving X to fragments are 350 instructions beside 40 matrix
+// instructions for 128 k of 64 x 32 outputs (3584 x 18,944, 61 rows, groups of 64, residual: 32 us, 0.26 PFLOP/s, 4.6 of them the launch that adds splits).
+//
+//   * The wavefronts of a workgroup divide K: a step is 128 k of the workgroup's rows of W, read in rows of 64 bytes and turned in LDS (fragments read as
+//     the matrix cores take them, a row a lane: 82 us for the first of these products, then 68), two steps under way in registers.
+//   * Scales and zeros of as many steps as fit lie in LDS: gathered from memory by every lane they cost as many cache lines as the codes.
 #include "common.h"
 
 #include <algorithm>
@@ -387,7 +398,9 @@ template <typename T, int G>
 int32_t launch_quant_shape(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
     constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;           // fp32 has one block of rows a workgroup
     if (p.mt == 2) return p.waves == 4 ? launch_quant<T, G, 4, kTwo, 4>(p, a, stream) : launch_quant<T, G, 4, kTwo, 8>(p, a, stream);
-    if (p.ns == 4) return p.waves == 4 ? launch_quant<T, G, 4, 1, 4>(p, a, stream) : launch_quant<T, G, 4, 1, 8>(p, a, stream);
+    if constexpr (sizeof(T) == 4)                          // more than 16 rows in 32 bits, too few tiles for the chip
+        if (p.ns == 4 && p.waves == 8) return launch_quant<T, G, 4, 1, 8>(p, a, stream);
+    if (p.ns == 4) return launch_quant<T, G, 4, 1, 4>(p, a, stream);
     return p.ns == 2 ? launch_quant<T, G, 2, 1, 8>(p, a, stream) : launch_quant<T, G, 1, 1, 8>(p, a, stream);
 }
 

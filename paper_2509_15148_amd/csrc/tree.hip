@@ -4,8 +4,8 @@
 // the same cached keys, and every row also reads the new rows it descends from.  z = scale q.k (or cap tanh(z / cap)), out = sum exp(z) v / sum exp(z)
 // in one pass over the keys, with a running maximum.  A few rows over a long context are bound by the cache's bytes (one row of 70B heads over 131,071
 // tokens: 100 us, 5.3 TB/s, the rate of a large copy); many rows by the vector unit, which takes an exponential a score, two with a cap (24 sequences of
-// 32B heads, up to 64 rows, cap and window: 161 us, 0.35 PFLOP/s); a single tree by the way of one workgroup from its first load to its last
-// barrier (16 rows of 7B heads over 512 tokens: 10.7 us).
+// 32B heads, up to 64 rows, cap and window: 156 us, 0.36 PFLOP/s); a single tree by the way of one workgroup from its first load to its last
+// barrier (16 rows of 7B heads over 512 tokens: 9.9 us).
 //
 //   * A wavefront holds up to 48 query rows (tiles of 16) and walks over tiles of 32 keys (16 in fp32).  S^T = K Q^T: the keys are the rows of the
 //     product, so lane (r = l % 16, c = l / 16) ends with scores of query row r only, of 8 (4) keys that lie one behind the other.  These are just
@@ -595,7 +595,7 @@ struct TreePlan {
 constexpr int64_t kTreePartRows = 1 << 16;                // (row, head, split) partial sums of a call that is cut
 
 // Keys that one workgroup takes faster than several do with the launch that joins them: 7B heads, 4 rows, 1020 tokens: 12.4 us, 13.1 in splits; 2040
-// tokens: 17.8 and 13.0.
+// tokens: 17.6 and 12.2.
 constexpr int64_t kTreeWhole = 1024;
 
 TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max_rows, int32_t max_cached, int32_t window) {
@@ -605,12 +605,12 @@ TreePlan tree_plan(const atts_paged_cache& c, int32_t nq, int32_t R, int32_t max
     const int64_t keys_per_tile = c.dtype == ATTS_DTYPE_F32 ? 16 : 32, slots = (int64_t)c.max_pages * c.page_rows;
     const int64_t keys = std::min((window ? std::min((int64_t)max_cached, (int64_t)window + 31) : max_cached) + (int64_t)max_rows, slots);
     // Row tiles of 48 read the cache a third as often as tiles of 16, whose shorter way is faster while each finds a compute unit of its own (7B heads,
-    // 16 rows, 520 tokens: 10.9 us with 16 and 16.2 with 48; 70B heads, 4 x 16 rows, 4090 tokens: 32 and 39, 30,000 tokens: 192 and 109; 32B heads,
-    // 4 x 32 rows, 1.25 tiles of 16 a unit, 4090 tokens: 57 and 35).  Heads of 256: the accumulators of 16 rows are what fits.
+    // 16 rows, 520 tokens: 10.0 us with 16 and 15.1 with 48; 70B heads, 4 x 16 rows, 4090 tokens: 33 and 33, 30,000 tokens: 241 and 141; 32B heads,
+    // 4 x 32 rows, 1.25 tiles of 16 a unit, 4090 tokens: 60 and 37).  Heads of 256: the accumulators of 16 rows are what fits.
     t.q_tiles = rows <= 16 || c.head_dim > 128 || (keys <= 4096 && heads * ceil_div(rows, 16) <= kChip) ? 1 : rows <= 32 ? 2 : 3;
     t.row_tiles = (int32_t)std::max<int64_t>(1, ceil_div(rows, 16 * t.q_tiles));
     // Splits fill what the compute units hold at a time, one workgroup of eight wavefronts or two of four, and not more (70B heads, 64 rows, 60,000 tokens,
-    // 88 tiles: 215 us with 5 splits and 258 with 6), of 256 keys or more.
+    // 88 tiles: 249 us with 5 splits and 273 with 6), of 256 keys or more.
     const int64_t room = (t.q_tiles == 1 ? kChip : 2 * kChip) / std::max<int64_t>(1, heads * t.row_tiles);
     const int64_t most = std::min(ceil_div(keys, 256), kTreePartRows / std::max<int64_t>(1, (int64_t)R * nq));
     const int64_t splits = keys <= kTreeWhole ? 1 : std::max<int64_t>(1, std::min(room, most));
