@@ -3,12 +3,13 @@
 // A group's sum is scale (sum_k (16 + code) x - (16 + zero) sum_k x): 16 + code is exact in 16 bits and costs one shift and one and-or for two codes, so
 // the matrix cores multiply codes with activations exactly, their product with a column of ones gives sum_k x, and the scale, 32 bits, comes once a
 // group.  In 32 bits x goes in as three 16-bit parts whose sum it is.  Every weight has to be read once, half a byte and its share of a scale; up to 16 rows
-// that is the bound (2 x 28,672 rows of W, K 8192, 16 rows, SwiGLU: 63 us, 3.9 TB/s, 78 % of a copy's rate; 4608 x 3584, one row: 6.6 us, an append of
+// that is the bound (2 x 28,672 rows of W, K 8192, 16 rows, SwiGLU: 63 us, 3.9 TB/s, 78 % of a copy's rate; 4608 x 3584, one row: 6.4 us, an append of
 // a few rows takes 5.7).  With more rows the vector unit is: unpacking, the groups' multiply-adds and moving X to fragments are 350 instructions beside 40 matrix
-// instructions for 128 k of 64 x 32 outputs (3584 x 18,944, 61 rows, groups of 64, residual: 32 us, 0.26 PFLOP/s, 4.6 of them the launch that adds splits).
+// instructions for 128 k of 64 x 32 outputs (3584 x 18,944, 61 rows, groups of 64, residual: 28.5 us, 0.29 PFLOP/s, 4.6 of them the launch that adds splits).
 //
 //   * The wavefronts of a workgroup divide K: a step is 128 k of the workgroup's rows of W, read in rows of 64 bytes and turned in LDS (fragments read as
-//     the matrix cores take them, a row a lane: 82 us for the first of these products, then 68), two steps under way in registers.
+//     the matrix cores take them, a row a lane: 82 us for the first of these products, then 68).  Up to 16 rows two steps are under way in registers; with two blocks
+//     of rows one, whose X passes through LDS in halves, which leaves registers and LDS for twelve wavefronts (61 rows: 32 us with eight and two steps, so 28.5).
 //   * Scales and zeros of as many steps as fit lie in LDS: gathered from memory by every lane they cost as many cache lines as the codes.
 #include "common.h"
 
@@ -106,16 +107,18 @@ __device__ __forceinline__ void swap_quarters(u32x4& w) {
 }
 
 // Wavefronts a SIMD is to hold: what the registers of a shape allow without spilling.
-template <typename T, int NS, int MT>
+template <typename T, int NS, int MT, int W>
 struct QuantWaves {
-    static constexpr int kN = NS == 4 ? (MT == 1 && sizeof(T) == 2 ? 3 : 2) : sizeof(T) == 2 ? (NS == 1 ? 5 : 4) : 3;
+    static constexpr int kN = NS == 4 ? (sizeof(T) == 2 && (MT == 1 || W == 12) ? 3 : 2) : sizeof(T) == 2 ? (NS == 1 ? 5 : 4) : 3;
 };
 
 // A workgroup's LDS: the turn of each wavefront, then scales, and behind the loop sums in their place.
 template <typename T, int G, int NS, int MT, int W>
 struct QuantLds {
     static constexpr int kGroups = kSpan / G, kScalePitch = 16 * NS + 1;
-    static constexpr int kTurn = W * (NS * 64 + MT * Parts<T>::kLoads * 256) * 16, kRed = W * 16 * (16 * NS + 4) * 4;
+    static constexpr bool kHalves = MT == 2;
+    static constexpr int kOwn = NS * 64 + MT * (kHalves ? 2 : 4) * Parts<T>::kLoads * 64;            // pieces of a wavefront: codes, X of half a step or a whole one
+    static constexpr int kTurn = W * kOwn * 16, kRed = W * 16 * (16 * NS + 4) * 4;
     static constexpr int kStep = kGroups * kScalePitch * (int)sizeof(typename Parts<T>::Scale);      // scales of a step
     static constexpr int kMost = kStageBytes / kStep / (2 * W) * (2 * W);                            // whole pairs of steps of every wavefront
     static_assert(kMost > 0);
@@ -126,7 +129,7 @@ struct QuantLds {
 // A workgroup: NS blocks of 16 weight rows (SwiGLU: gate and up blocks in turn) times MT blocks of 16 rows of X, over one split of K; its wavefronts
 // take every W-th step.  G: group size.
 template <typename T, int G, int NS, int MT, int W>
-__global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_kernel(QuantArgs a) {
+__global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT, W>::kN)) void quant_kernel(QuantArgs a) {
     using P = Parts<T>;
     constexpr int kGroups = kSpan / G, kRows = 16 * MT, kCols = 16 * NS, kPitch = kCols + 4;
     // Scales and zeros of as many steps as fit, [group][weight row]: a lane's own, two bytes of a row each, would cost as many cache lines a step as
@@ -152,35 +155,53 @@ __global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_ker
         return min(n, a.N - 1) + (swiglu ? (int64_t)(s & 1) * a.N : 0);     // the block itself may lie behind the end
     };
     const auto last_row = [&](int s) { return max(0, a.N - 1 - (swiglu ? tile * (kCols / 2) + s / 2 * 16 : tile * kCols + s * 16)); };
-    // Memory is read by rows: four lanes a weight row (64 bytes), kXLanes a row of X, so that neighbours share a cache line.
-    constexpr int kXLanes = kSpan * sizeof(T) / 16, kXLoads = 16 * kXLanes / 64;
+    // Memory is read by rows, four lanes 64 bytes of codes, so that neighbours share a cache line.  X: with one block of rows kXLanes lanes a whole row; with
+    // two, halves of a step pass through LDS one after the other, which leaves room for 12 wavefronts, four lanes 64 bytes (kHalves).
+    constexpr bool kHalves = L::kHalves;
+    constexpr int kXLanes = kSpan * sizeof(T) / 16, kXLoads = kHalves ? 1 : 16 * kXLanes / 64;
+    const int quarter = lane & 3, row16 = lane >> 2;
     int64_t first[NS];
     uint32_t at_w[NS], at_x[MT][kXLoads];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         first[s] = first_row(s);
-        at_w[s] = (uint32_t)min(lane >> 2, last_row(s)) * (uint32_t)(a.K / 2);
+        at_w[s] = (uint32_t)min(row16, last_row(s)) * (uint32_t)(a.K / 2);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i)
-            at_x[m][i] = (uint32_t)min(m * 16 + (i * 64 + lane) / kXLanes, a.M - 1 - m0) * (uint32_t)(a.x_stride * sizeof(T));
+            at_x[m][i] = (uint32_t)min(m * 16 + (kHalves ? row16 : (i * 64 + lane) / kXLanes), a.M - 1 - m0) * (uint32_t)(a.x_stride * sizeof(T));
     const char* const x0 = reinterpret_cast<const char*>(a.x) + m0 * a.x_stride * (int64_t)sizeof(T);
 
     struct Step {
-        u32x4 w[NS], x[MT][kXLoads];
+        u32x4 w[NS], x[MT][4][P::kLoads];
     };
-    auto load = [&](Step& f, int t) __attribute__((always_inline)) {
-        const int k = min(t, t1 - 1) * kSpan;                               // past the end: a repeat, not used
-        const uint32_t own_w = k + (lane & 3) * 32 < a.K ? (lane & 3) * 16 : 0;     // a last step may be partly filled
-        const uint32_t own_x = k + lane % kXLanes * (16 / (int)sizeof(T)) < a.K ? lane % kXLanes * 16 : 0;
+    // Past the end, and in a last step that is partly filled: a repeat, not used.
+    auto load_codes = [&](Step& f, int t) __attribute__((always_inline)) {
+        const int k = min(t, t1 - 1) * kSpan;
+        const uint32_t own_w = k + quarter * 32 < a.K ? quarter * 16 : 0;
 #pragma unroll
         for (int s = 0; s < NS; ++s) f.w[s] = *reinterpret_cast<const u32x4*>(a.codes + first[s] * (a.K / 2) + k / 2 + (at_w[s] + own_w));
+    };
+    auto load_x = [&](Step& f, int t, int half) __attribute__((always_inline)) {
+        const int k = min(t, t1 - 1) * kSpan;
+        const uint32_t own_x = k + lane % kXLanes * (16 / (int)sizeof(T)) < a.K ? lane % kXLanes * 16 : 0;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int i = 0; i < kXLoads; ++i) f.x[m][i] = *reinterpret_cast<const u32x4*>(x0 + (int64_t)k * sizeof(T) + (at_x[m][i] + own_x));
+            for (int j = 2 * half; j < 2 * half + 2; ++j)
+#pragma unroll
+                for (int i = 0; i < P::kLoads; ++i) {
+                    if constexpr (kHalves)
+                        f.x[m][j][i] = *reinterpret_cast<const u32x4*>(x0 + (int64_t)(k + j * 32 < a.K ? k + j * 32 : 0) * sizeof(T) + i * 64 + (at_x[m][0] + quarter * 16));
+                    else f.x[m][j][i] = *reinterpret_cast<const u32x4*>(x0 + (int64_t)k * sizeof(T) + (at_x[m][j * P::kLoads + i] + own_x));
+                }
+    };
+    auto load = [&](Step& f, int t) __attribute__((always_inline)) {
+        load_codes(f, t);
+        load_x(f, t, 0);
+        load_x(f, t, 1);
     };
     f32x4 acc[NS][MT];
 #pragma unroll
@@ -192,31 +213,46 @@ __global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_ker
     asm("s_mov_b32 %0, 0x00780078" : "=s"(mask));
     asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
     int staged = 0;                                                         // first step whose scales are in LDS
-    auto products = [&](Step& f, int t, auto whole) __attribute__((always_inline)) {
+    // One step, in f; kHalves: and the request for step `next` once what it takes the place of is in LDS.
+    auto products = [&](Step& f, int t, auto whole, int next) __attribute__((always_inline)) {
         const typename P::Scale* mine = lds_scale + (t - staged) * kGroups * kScalePitch + r;
         // Rows to fragments through LDS; a wavefront's accesses to it are done in their order, so nothing has to be waited for between them.  A
         // piece of 16 bytes lies where eight rows' pieces that are read together fall into different banks.
-        u32x4* const own = turn + wave * (NS * 64 + MT * P::kLoads * 256);
+        constexpr int kPieces = 4 * P::kLoads;                              // of 32 k of a row of X
+        u32x4* const own = turn + wave * L::kOwn;
         u32x4* const own_x = own + NS * 64;
+        const auto spread = [](int row) { return P::kLoads == 1 ? row >> 1 & 3 : row & 7; };
 #pragma unroll
-        for (int s = 0; s < NS; ++s) own[s * 64 + (lane & ~3) + ((lane & 3) ^ (lane >> 3 & 3))] = f.w[s];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < kXLoads; ++i) {
-                const int row = (i * 64 + lane) / kXLanes;
-                own_x[(m * 16 + row) * kXLanes + (lane % kXLanes ^ (row & 7))] = f.x[m][i];
-            }
+        for (int s = 0; s < NS; ++s) own[s * 64 + (lane & ~3) + (quarter ^ (lane >> 3 & 3))] = f.w[s];
+        if (kHalves && decltype(whole)::value) load_codes(f, next);
         u32x4 code[NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             code[s] = own[s * 64 + r * 4 + (c ^ (r >> 1 & 3))];
-            if (G < kSpan) swap_quarters(code[s]);
+            if (kHalves || G < kSpan) swap_quarters(code[s]);
         }
         f32x4 sum[NS][MT], sx[MT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (!decltype(whole)::value && t * kSpan + j * 32 >= a.K) break;    // wave-uniform
+            if (kHalves && j % 2 == 0) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                        for (int i = 0; i < P::kLoads; ++i) own_x[((m * 2 + jj) * 16 + row16) * kPieces + ((i * 4 + quarter) ^ spread(row16))] = f.x[m][j + jj][i];
+                if (decltype(whole)::value) load_x(f, next, j / 2);
+            }
+            if (!kHalves && j == 0) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4 * P::kLoads; ++i) {
+                        const int row = (i * 64 + lane) / kXLanes;
+                        own_x[(m * 16 + row) * kXLanes + (lane % kXLanes ^ (row & 7))] = f.x[m][i / P::kLoads][i % P::kLoads];
+                    }
+            }
             if (j * 32 % G == 0) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
@@ -234,7 +270,8 @@ __global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_ker
 #pragma unroll
                 for (int i = 0; i < P::kLoads; ++i) {
                     const int piece = (G < kSpan ? 4 * j + c : 4 * c + j) * P::kLoads + i;
-                    raw[i] = own_x[(m * 16 + r) * kXLanes + (piece ^ (r & 7))];
+                    raw[i] = kHalves ? own_x[((m * 2 + j % 2) * 16 + r) * kPieces + ((c * P::kLoads + i) ^ spread(r))]
+                                     : own_x[(m * 16 + r) * kXLanes + (piece ^ (r & 7))];
                 }
                 const P part(raw);
 #pragma unroll
@@ -268,38 +305,40 @@ __global__ __launch_bounds__(64 * W, (QuantWaves<T, NS, MT>::kN)) void quant_ker
             uint8_t zero[kEach];
 #pragma unroll
             for (int u = 0; u < kEach; ++u) {
-                const int i = wave + u * W, s = i >> 4;           // rows past the last one repeat it
+                const int i = kCols % W ? min(wave + u * W, kCols - 1) : wave + u * W, s = i >> 4;           // rows past the last one repeat it
                 const int64_t at = (first_row(s) + min(i & 15, last_row(s))) * a.groups + from * kGroups + g;
                 scale[u] = reinterpret_cast<const T*>(a.scales)[at];
                 zero[u] = zeros[at];
             }
 #pragma unroll
             for (int u = 0; u < kEach; ++u)
-                if (g0 + lane < n) lds_scale[g * kScalePitch + wave + u * W] = P::pack(scale[u], a.zeros ? zero[u] : 8);
+                if (g0 + lane < n && (kCols % W == 0 || wave + u * W < kCols)) lds_scale[g * kScalePitch + wave + u * W] = P::pack(scale[u], a.zeros ? zero[u] : 8);
         }
     };
 
-    // Two steps are under way in two sets of registers.  The loop has no branch inside, or the waits would be for everything; what does not make
-    // a pair of whole steps is left for the end.
-    Step fa, fb;
+    // The loop has no branch inside, or the waits would be for everything; a step that is partly filled is left for the end.  One block of rows: two steps
+    // under way in two sets of registers; two blocks: one, and more wavefronts.
+    constexpr int kSets = MT == 1 ? 2 : 1;
+    Step f[kSets];
     int t = t0 + wave;
-    load(fa, t);
-    load(fb, t + W);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) load(f[i], t + i * W);
     for (int from = t0; from < t1; from += a.stage_steps) {
         const int end = min(from + a.stage_steps, t1), whole = min(end, a.K / kSpan);
         if (from > t0) __syncthreads();
         stage(from, end - from);
         staged = from;
         __syncthreads();
-        for (; t + W < whole; t += 2 * W) {
-            products(fa, t, std::true_type{});
-            load(fa, t + 2 * W);
-            products(fb, t + W, std::true_type{});
-            load(fb, t + 3 * W);
-        }
+        for (; t + (kSets - 1) * W < whole; t += kSets * W)
+#pragma unroll
+            for (int i = 0; i < kSets; ++i) {
+                products(f[i], t + i * W, std::true_type{}, t + (i + kSets) * W);
+                if (!kHalves) load(f[i], t + (i + kSets) * W);
+            }
     }
-    if (t < t1) products(fa, t, std::false_type{});
-    if (t + W < t1) products(fb, t + W, std::false_type{});
+#pragma unroll
+    for (int i = 0; i < kSets; ++i)
+        if (t + i * W < t1) products(f[i], t + i * W, std::false_type{}, 0);
     __syncthreads();
 
     // acc[s][m][i]: row 4 c + i of block m, column r of block s.  The wavefronts' sums are added in their order.
@@ -363,12 +402,13 @@ QuantPlan quant_plan(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t epi
     p.row_blocks = (int32_t)ceil_div(M, 16 * p.mt);
     // Tiles of 64 weight rows read X least often.  With at most 16 rows of X narrower ones follow where those would leave compute units without
     // work: 32 from half a workgroup a unit on, else 16 (16 rows, K 27,648: N 5120 45 us with tiles of 16 and 35 with 32; 1 row, K 18,944: N 3584
-    // 19 and 25).  More rows keep the wide tiles and divide K, first among eight wavefronts instead of four, then over workgroups (24 rows,
-    // N 3584, K 18,944: 25 us with 4 splits, 55 with one; where the tiles fill the chip four wavefronts are faster: 64 rows, N 10,240, K 8192: 41 and 46).
+    // 19 and 25).  More rows keep the wide tiles and divide K, first among twelve wavefronts instead of four, then over workgroups (24 rows,
+    // N 3584, K 18,944: 24 us with 4 splits and twelve, 27 with four; 55 with neither; 40 rows, K 8192: N 8192, a tile a unit, 32 and 39; where the tiles are
+    // more four wavefronts are faster, so that several workgroups share a unit: 64 rows, N 10,240, K 8192: 39 and 43).
     p.ns = M > 16 || ceil_div(wide, 64) >= kChip ? 4 : swiglu || ceil_div(wide, 32) >= kChip / 2 ? 2 : 1;
     p.tiles = (int32_t)(swiglu ? ceil_div(N, 8 * p.ns) : ceil_div(wide, 16 * p.ns));
     const int64_t cells = (int64_t)p.tiles * p.row_blocks;
-    p.waves = p.ns == 4 && cells >= kChip ? 4 : 8;
+    p.waves = p.mt == 2 ? (cells > kChip ? 4 : 12) : p.ns == 4 && cells >= kChip ? 4 : 8;
     p.steps = (int32_t)ceil_div(K, kSpan);
     const int64_t splits = M <= 16 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kChip / cells, p.steps / 4));
     p.steps_per_split = (int32_t)ceil_div(p.steps, splits);
@@ -396,8 +436,8 @@ int32_t launch_quant(const QuantPlan& p, QuantArgs a, hipStream_t stream) {
 
 template <typename T, int G>
 int32_t launch_quant_shape(const QuantPlan& p, const QuantArgs& a, hipStream_t stream) {
-    constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;           // fp32 has one block of rows a workgroup
-    if (p.mt == 2) return p.waves == 4 ? launch_quant<T, G, 4, kTwo, 4>(p, a, stream) : launch_quant<T, G, 4, kTwo, 8>(p, a, stream);
+    if constexpr (sizeof(T) == 2)                          // fp32 has one block of rows a workgroup
+        if (p.mt == 2) return p.waves == 4 ? launch_quant<T, G, 4, 2, 4>(p, a, stream) : launch_quant<T, G, 4, 2, 12>(p, a, stream);
     if constexpr (sizeof(T) == 4)                          // more than 16 rows in 32 bits, too few tiles for the chip
         if (p.ns == 4 && p.waves == 8) return launch_quant<T, G, 4, 1, 8>(p, a, stream);
     if (p.ns == 4) return launch_quant<T, G, 4, 1, 4>(p, a, stream);

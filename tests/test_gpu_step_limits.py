@@ -63,6 +63,14 @@ def test_wide_few_rows_and_many_rows(dtype, M, N, K, group, epilogue):
     check_product(*inputs, epilogue, run_product(*inputs, epilogue, N))
 
 
+@pytest.mark.parametrize("M,N,K,group", [(20, 8200, 4128, 32), (40, 8200, 5152, 32), (20, 8200, 7232, 64), (10, 16500, 4128, 32)])
+def test_scales_brought_in_parts(M, N, K, group):
+    """More groups than LDS holds the scales of at a time, a last step that is partly filled."""
+    announce("quant many groups", M, N, K, group)
+    inputs = product_inputs(M, N, K, group, True, "store_f32", torch.bfloat16, M + N)
+    check_product(*inputs, "store_f32", run_product(*inputs, "store_f32", N))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_a_workspace_of_the_caller_s(dtype):
     inputs = product_inputs(33, 100, 4096, 64, True, "store", dtype, 2)
