@@ -14,7 +14,7 @@
 //   * The logits of the next row are requested before those of this one are used; results stay in registers for the maximum and the sum of
 //     exponentials: one read and one write of the logits.  Every wavefront leaves (maximum, its index, sum) of its part; a second launch joins the
 //     parts of a row in a fixed order.
-//   * Slices of 1024 (16 bits: 2048) tokens spread a few rows, of 4096 more; slices of 16,384 or 32,768 read a long history less often (logits_plan).
+//   * Slices of 1024 (16 bits: 2048) tokens spread a few rows, of 4096 more; slices of 8192 or 16,384 read a long history less often (logits_plan).
 #include "lanes.h"
 #include "paged.h"
 
@@ -360,11 +360,11 @@ LogitsPlan logits_plan(int32_t dtype, int32_t R, int32_t n_seqs, int32_t max_row
         return p;
     }
     p.tokens = kTokens;
-    // Every slice reads the whole history: with many sequences of long ones larger slices cost less than what smaller ones gain by running side by side
-    // (128,256 logits in 16 bits, 256 rows, histories of 16,000 on average: 74 us with slices of 32,768, 81 with 16,384, 93 with 4096; 152,064 logits in 32
-    // bits, 256 rows: 105, 119 and 130, with histories of 1000 91, 100 and 83; 64 x 4 rows, histories of 4000: 97, 90 and 82).
-    p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 && n_history / n_seqs >= 8192 ? 1024 : 256;
-    p.passes = p.threads == 1024 && counts && !bias ? 2 : 1;                  // with biases too, two rounds' tables do not fit the LDS
+    // Every slice reads the whole history: with many sequences of long ones slices of 512 threads and two rounds, two workgroups a unit, cost less than what
+    // smaller ones gain by running side by side (152,064 logits in 16 bits, histories of 16,000 on average: 128 rows 48 us, 59 with 256 threads, 53 with
+    // 1024; 256 rows 89, 112 and 94; with histories of 1000 77 and 69 with 256; 64 x 4 rows in 32 bits, histories of 4000: 86 and 82).
+    p.threads = (int64_t)n_seqs * ceil_div(V, 256 * kTokens) >= 1024 && n_history / n_seqs >= 8192 ? 512 : 256;
+    p.passes = p.threads == 512 && counts && !bias ? 2 : 1;                   // with biases too, tables of two rounds would leave a unit one workgroup
     p.slices = (int32_t)ceil_div(V, p.threads * kTokens * p.passes);
     const int64_t cells = (int64_t)n_seqs * p.slices, chunks = std::min<int64_t>(max_rows, std::max<int64_t>(1, 1536 / std::max<int64_t>(1, cells)));
     p.rows_per_wg = (int32_t)ceil_div(max_rows, chunks);
@@ -373,9 +373,9 @@ LogitsPlan logits_plan(int32_t dtype, int32_t R, int32_t n_seqs, int32_t max_row
 
 template <typename T, int VEC, int THREADS, int PASSES, int TOKENS>
 int32_t launch_logits(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
-    constexpr size_t table = (size_t)THREADS * TOKENS * PASSES * 4;
-    constexpr bool both = 2 * table <= 160 * 1024 - 4096;
-    const int32_t rc = allow_dynamic_lds<logits_kernel<T, VEC, THREADS, PASSES, TOKENS>>((both ? 2 * table : table) + 256);
+    constexpr size_t table = (size_t)THREADS * TOKENS * PASSES * 4;           // of counts, and of biases
+    static_assert(2 * table + 256 <= 160 * 1024 - 4096);
+    const int32_t rc = allow_dynamic_lds<logits_kernel<T, VEC, THREADS, PASSES, TOKENS>>(2 * table + 256);
     if (rc != ATTS_OK) return rc;
     hipLaunchKernelGGL((logits_kernel<T, VEC, THREADS, PASSES, TOKENS>), dim3((unsigned)p.slices, (unsigned)ceil_div(a.max_rows, p.rows_per_wg), (unsigned)n_seqs),
                        dim3(THREADS), (a.params ? table + 256 : 0) + (a.bias_ids ? table : 0), stream, static_cast<const T*>(logits), static_cast<T*>(out), a);
@@ -387,8 +387,8 @@ template <typename T, int VEC>
 int32_t launch_logits_shape(const LogitsPlan& p, const LogitsArgs& a, int32_t n_seqs, const void* logits, void* out, hipStream_t stream) {
     if (p.tokens == kShort<T>) return launch_logits<T, VEC, 256, 1, kShort<T>>(p, a, n_seqs, logits, out, stream);
     if (p.threads == 256) return launch_logits<T, VEC, 256, 1, kTokens>(p, a, n_seqs, logits, out, stream);
-    return p.passes == 2 ? launch_logits<T, VEC, 1024, 2, kTokens>(p, a, n_seqs, logits, out, stream)
-                         : launch_logits<T, VEC, 1024, 1, kTokens>(p, a, n_seqs, logits, out, stream);
+    return p.passes == 2 ? launch_logits<T, VEC, 512, 2, kTokens>(p, a, n_seqs, logits, out, stream)
+                         : launch_logits<T, VEC, 512, 1, kTokens>(p, a, n_seqs, logits, out, stream);
 }
 
 template <typename T>
