@@ -2,8 +2,8 @@
 // keys and values.
 //
 // A pair (a, b) of a head turns to (a c - b s, b c + a s), with c and s of the row's position from the table, in 32 bits, rounded once.  Every element is
-// read and written once; a prompt is bound by that (4093 rows of 70B heads, 169 MB: 46 us, 3.7 TB/s, a copy of as many bytes takes 33), a step of a few rows by
-// one launch (16 rows of 7B heads: 5.7 us) and the way row -> sequence -> page -> slot (58 rows in 5 trees: 7.5 us).
+// read and written once; a prompt is bound by that (4093 rows of 70B heads, 169 MB: 40 us, 4.2 TB/s, a copy of as many bytes takes 33), a step of a few rows by
+// one launch (16 rows of 7B heads: 5.3 us) and the way row -> sequence -> page -> slot (58 rows in 5 trees: 7.5 us).
 #include "paged.h"
 
 #include <math.h>
@@ -57,8 +57,12 @@ struct AppendArgs {
     const float2* table;
     int64_t qkv_stride;
     int32_t R, nq, n_positions, half, interleaved;
-    int32_t heads_each, turned_chunks, values_each;      // set by launch_append: heads of a workgroup, chunks of query and key heads
+    int32_t turned_chunks;                               // set by launch_append: chunks of kHeads query and key heads
 };
+
+// Query and key heads of a workgroup, for which the table's rows are read once (4093 rows of 70B heads: 45 us, 67 with one head, 54 with eight; 500 rows 15, 16
+// and 16), and value elements of one: whole heads of 128 were the longest way through the launch (4093 rows 45 us, 42 in parts; 500 rows 15 and 11).
+constexpr int kHeads = 4, kValues = 32;
 
 // Rows r0 .. r0 + n - 1 (n <= 64) of a workgroup: each one's token and page in its sequence's cache, page -1 if it has none.  By one wavefront: the
 // sequences of the first and the last row by a search of the whole wavefront, of those between by counting offsets.
@@ -89,7 +93,7 @@ struct Places {
     }
 };
 
-// A workgroup: 64 rows, and a few query and key heads or (the last ones of a grid's y) a few value heads.
+// A workgroup: 64 rows, and a few query and key heads or (the last ones of a grid's y) a part of a value head.
 //   * Queries and keys: a thread keeps the cosines and sines of its piece of a row for all its heads.  PIECE elements are 16 bytes; a piece of the first
 //     half turns with its partner half a rotation on (or within itself, interleaved).
 //   * Values go through LDS: a thread gathers the tokens of one head element that lie side by side in the page and writes 16 bytes of them;
@@ -101,12 +105,12 @@ __global__ __launch_bounds__(256) void rotary_append_kernel(const T* __restrict_
     typedef T Vec __attribute__((ext_vector_type(PIECE)));
     constexpr int kGroup = 16 / sizeof(T);               // tokens of a 16-byte store
     __shared__ Places places;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ T tile[64][kValues + 1];                  // an odd pitch, so that rows eight apart fall into different banks
     const int tid = threadIdx.x, r0 = blockIdx.x * 64, n = min(64, a.R - r0), hd = p.hd, turned = a.nq + p.n_kv;
-    const int first = (int)blockIdx.y * a.heads_each;
+    const int first = (int)blockIdx.y * kHeads;
     const bool values = (int)blockIdx.y >= a.turned_chunks;
     if (!values) {
-        const int last = min(first + a.heads_each, turned), rot = 2 * a.half;
+        const int last = min(first + kHeads, turned), rot = 2 * a.half;
         if (last > a.nq) {                                   // the workgroup has keys
             if (tid < 64) places.find(p, a, r0, n, tid);
             __syncthreads();
@@ -120,13 +124,20 @@ __global__ __launch_bounds__(256) void rotary_append_kernel(const T* __restrict_
             const float2* cs = a.table + (int64_t)min(max(a.positions[r], 0), a.n_positions - 1) * a.half;
             const bool inside = a.interleaved && PIECE > 1 && e < rot;
             float c[PIECE], s[PIECE];
+            if (pair) {
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) {
-                float2 t = make_float2(1.f, 0.f);
-                if (pair) t = cs[e + j];
-                else if (inside && e + j < rot) t = cs[(e + j) >> 1];
-                c[j] = t.x;
-                s[j] = t.y;
+                for (int j = 0; j < PIECE; ++j) {
+                    const float2 t = cs[e + j];
+                    c[j] = t.x;
+                    s[j] = t.y;
+                }
+            } else if (inside) {                             // whole: 2 half is a multiple of PIECE
+#pragma unroll
+                for (int j = 0; j < PIECE; j += 2) {
+                    const float2 t = cs[(e + j) >> 1];
+                    c[j] = t.x;
+                    s[j] = t.y;
+                }
             }
             const T* src = qkv + (int64_t)r * a.qkv_stride;
 #pragma unroll 4
@@ -175,42 +186,38 @@ __global__ __launch_bounds__(256) void rotary_append_kernel(const T* __restrict_
     }
     if (tid < 64) places.find(p, a, r0, n, tid);
     __syncthreads();
-    T* const tile = reinterpret_cast<T*>(smem);              // [64][hd + 1]: an odd pitch, so that rows eight apart fall into different banks
-    const int pitch = hd + 1, h0 = ((int)blockIdx.y - a.turned_chunks) * a.values_each, h1 = min(h0 + a.values_each, p.n_kv);
+    const int parts = (hd + kValues - 1) / kValues, chunk = (int)blockIdx.y - a.turned_chunks, h = chunk / parts, d0 = chunk % parts * kValues, nd = min(kValues, hd - d0);
     // groups of rows begin where the first row's page has a 16-byte place
     const int lead = (kGroup - places.token[0] % kGroup) % kGroup, groups = (n - lead + kGroup - 1) / kGroup + (lead > 0);
-    for (int h = h0; h < h1; ++h) {
-        if (h > h0) __syncthreads();
-        for (int item = tid; item < n * hd / PIECE; item += 256) {
-            const int i = item / (hd / PIECE), e = (item - i * (hd / PIECE)) * PIECE;
-            const T* from = qkv + (int64_t)(r0 + i) * a.qkv_stride + (int64_t)(turned + h) * hd + e;
-            if constexpr (PIECE == 1) tile[i * pitch + e] = *from;
-            else {
-                const Vec x = *reinterpret_cast<const Vec*>(from);
+    for (int item = tid; item < n * nd / PIECE; item += 256) {
+        const int i = item / (nd / PIECE), e = (item - i * (nd / PIECE)) * PIECE;
+        const T* from = qkv + (int64_t)(r0 + i) * a.qkv_stride + (int64_t)(turned + h) * hd + d0 + e;
+        if constexpr (PIECE == 1) tile[i][e] = *from;
+        else {
+            const Vec x = *reinterpret_cast<const Vec*>(from);
 #pragma unroll
-                for (int j = 0; j < PIECE; ++j) tile[i * pitch + e + j] = x[j];
-            }
+            for (int j = 0; j < PIECE; ++j) tile[i][e + j] = x[j];
         }
-        __syncthreads();
-        for (int item = tid; item < groups * hd; item += 256) {
-            const int d = item / groups, g = item - d * groups;
-            const int i0 = lead > 0 ? (g ? lead + (g - 1) * kGroup : 0) : g * kGroup, i1 = min(lead > 0 && g == 0 ? lead : i0 + kGroup, n);
-            const int page = places.page[i0], token = places.token[i0];
-            // a whole place: kGroup tokens of one page, one behind the other (page sizes are multiples of it)
-            bool whole = i1 - i0 == kGroup && page >= 0 && token % kGroup == 0;
-            if (whole) whole = places.page[i0 + kGroup - 1] == page && places.token[i0 + kGroup - 1] == token + kGroup - 1;
-            if (whole)
-                for (int i = i0 + 1; i < i1 - 1; ++i) whole &= places.page[i] == page && places.token[i] == token + i - i0;
-            if (whole) {
-                typedef T Group __attribute__((ext_vector_type(kGroup)));
-                Group y;
+    }
+    __syncthreads();
+    for (int item = tid; item < groups * nd; item += 256) {
+        const int d = item / groups, g = item - d * groups;
+        const int i0 = lead > 0 ? (g ? lead + (g - 1) * kGroup : 0) : g * kGroup, i1 = min(lead > 0 && g == 0 ? lead : i0 + kGroup, n);
+        const int page = places.page[i0], token = places.token[i0];
+        // a whole place: kGroup tokens of one page, one behind the other (page sizes are multiples of it)
+        bool whole = i1 - i0 == kGroup && page >= 0 && token % kGroup == 0;
+        if (whole) whole = places.page[i0 + kGroup - 1] == page && places.token[i0 + kGroup - 1] == token + kGroup - 1;
+        if (whole)
+            for (int i = i0 + 1; i < i1 - 1; ++i) whole &= places.page[i] == page && places.token[i] == token + i - i0;
+        if (whole) {
+            typedef T Group __attribute__((ext_vector_type(kGroup)));
+            Group y;
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j) y[j] = tile[(i0 + j) * pitch + d];
-                *reinterpret_cast<Group*>(v_pages + p.value_at(page, h, token) + ((int64_t)d << p.page_log)) = y;
-            } else {
-                for (int i = i0; i < i1; ++i)
-                    if (places.page[i] >= 0) v_pages[p.value_at(places.page[i], h, places.token[i]) + ((int64_t)d << p.page_log)] = tile[i * pitch + d];
-            }
+            for (int j = 0; j < kGroup; ++j) y[j] = tile[i0 + j][d];
+            *reinterpret_cast<Group*>(v_pages + p.value_at(page, h, token) + ((int64_t)(d0 + d) << p.page_log)) = y;
+        } else {
+            for (int i = i0; i < i1; ++i)
+                if (places.page[i] >= 0) v_pages[p.value_at(places.page[i], h, places.token[i]) + ((int64_t)(d0 + d) << p.page_log)] = tile[i][d];
         }
     }
 }
@@ -219,24 +226,17 @@ template <typename T>
 int32_t launch_append(const atts_paged_cache& c, const void* qkv, void* q_out, const PagedView& p, AppendArgs a, hipStream_t stream) {
     constexpr int kPiece = 16 / sizeof(T);
     const int64_t blocks = ceil_div(a.R, 64), turned = (int64_t)a.nq + p.n_kv;
-    // about four workgroups a compute unit: with fewer rows a head each, with many the table's rows are read once for several heads
-    a.heads_each = (int32_t)(turned * blocks / 1024 < 1 ? 1 : turned * blocks / 1024 > 16 ? 16 : turned * blocks / 1024);
-    a.turned_chunks = (int32_t)ceil_div(turned, a.heads_each);
-    a.values_each = 1;
+    a.turned_chunks = (int32_t)ceil_div(turned, kHeads);
     const bool pieces = !(((uintptr_t)qkv | (uintptr_t)q_out | (uint64_t)a.qkv_stride * sizeof(T)) & 15) && a.half % (a.interleaved ? 1 : kPiece) == 0 &&
                         (!a.interleaved || 2 * a.half % kPiece == 0);
-    const dim3 grid((unsigned)blocks, (unsigned)(a.turned_chunks + ceil_div(p.n_kv, a.values_each)));
-    const size_t lds = (size_t)64 * (p.hd + 1) * sizeof(T);
-    const auto run = [&](auto kernel, int32_t allowed) {
-        if (allowed != ATTS_OK) return allowed;
-        hipLaunchKernelGGL(kernel, grid, dim3(256), lds, stream, static_cast<const T*>(qkv), static_cast<T*>(q_out), static_cast<T*>(c.k_pages),
+    const dim3 grid((unsigned)blocks, (unsigned)(a.turned_chunks + p.n_kv * ceil_div(p.hd, kValues)));
+    const auto run = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, static_cast<const T*>(qkv), static_cast<T*>(q_out), static_cast<T*>(c.k_pages),
                            static_cast<T*>(c.v_pages), p, a);
         ATTS_LAUNCH_CHECK("rotary_append_kernel");
         return (int32_t)ATTS_OK;
     };
-    constexpr size_t most = 64 * 257 * sizeof(T);
-    return pieces ? run(rotary_append_kernel<T, kPiece>, allow_dynamic_lds<rotary_append_kernel<T, kPiece>>(most))
-                  : run(rotary_append_kernel<T, 1>, allow_dynamic_lds<rotary_append_kernel<T, 1>>(most));
+    return pieces ? run(rotary_append_kernel<T, kPiece>) : run(rotary_append_kernel<T, 1>);
 }
 
 }  // namespace
@@ -288,7 +288,7 @@ int32_t atts_rotary_append(const atts_paged_cache* cache, const void* qkv, int64
     if (rot_dim > 0 && (!table || ((uintptr_t)table & 7) || n_positions < 1)) return fail(ATTS_ERR_INVALID_ARG, "%s: table NULL, empty or not 8-byte aligned", fn);
     if (qkv_stride < (int64_t)(n_q_heads + 2 * p.n_kv) * p.hd) return fail(ATTS_ERR_INVALID_ARG, "%s: rows of qkv overlap", fn);
     const AppendArgs a{positions, cached, row_offsets, reinterpret_cast<const float2*>(table), qkv_stride, R, n_q_heads,
-                       n_positions < 1 ? 1 : n_positions, rot_dim / 2, layout == ATTS_ROTARY_INTERLEAVED, 0, 0, 0};
+                       n_positions < 1 ? 1 : n_positions, rot_dim / 2, layout == ATTS_ROTARY_INTERLEAVED, 0};
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return cache->dtype == ATTS_DTYPE_F32 ? launch_append<float>(*cache, qkv, q_out, p, a, stream) : launch_append<bf16>(*cache, qkv, q_out, p, a, stream);
 }

@@ -4,7 +4,7 @@
 // the matrix cores multiply codes with activations exactly, their product with a column of ones gives sum_k x, and the scale, 32 bits, comes once a
 // group.  In 32 bits x goes in as three 16-bit parts whose sum it is.  Every weight has to be read once, half a byte and its share of a scale; up to 16 rows
 // that is the bound (2 x 28,672 rows of W, K 8192, 16 rows, SwiGLU: 63 us, 3.9 TB/s, 78 % of a copy's rate; 4608 x 3584, one row: 6.4 us, an append of
-// a few rows takes 5.7).  With more rows the vector unit is: unpacking, the groups' multiply-adds and moving X to fragments are 350 instructions beside 40 matrix
+// a few rows takes 5.3).  With more rows the vector unit is: unpacking, the groups' multiply-adds and moving X to fragments are 350 instructions beside 40 matrix
 // instructions for 128 k of 64 x 32 outputs (3584 x 18,944, 61 rows, groups of 64, residual: 28.5 us, 0.29 PFLOP/s, 4.6 of them the launch that adds splits).
 //
 //   * The wavefronts of a workgroup divide K: a step is 128 k of the workgroup's rows of W, read in rows of 64 bytes and turned in LDS (fragments read as
